@@ -50,8 +50,9 @@ typedef enum {
     GRPO_ERR_PARAM = 5,     /* temperature <= 0, eps out of range, delta <= 1+eps_high */
     GRPO_ERR_WORKSPACE = 6, /* workspace NULL, misaligned or too small                 */
     GRPO_ERR_HIP = 7,       /* the HIP runtime reported an error at launch             */
-    GRPO_ERR_CAPACITY = 8   /* more rows than the library's built-in scratch array holds
+    GRPO_ERR_CAPACITY = 8,  /* more rows than the library's built-in scratch array holds
                                (grpo_loss_fwd_bwd_noalloc only)                         */
+    GRPO_ERR_OVERLAP = 9    /* arrays that must be apart share memory                   */
 } grpo_status;
 
 typedef enum {
@@ -462,6 +463,157 @@ grpo_status grpo_lmhead_loss_aux_fwd_bwd(const void *hidden, int64_t hidden_stri
                                          void *grad_hidden, int64_t grad_hidden_stride, float *grad_weight,
                                          int64_t grad_weight_stride, int accumulate_grad_weight,
                                          void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------- *
+ * The norms around a block of the model, with the block's gate and the scale it is added
+ * to the residual stream with: the block's output f is normed, weighted, gated, scaled and
+ * added, and the sum is normed for what follows (the next block, or the head: h is
+ * grpo_lmhead_loss_fwd_bwd's `hidden`, and its grad_hidden is what the backward takes).
+ *
+ *   x' = x + s g (.) f r1 (.) w1     r1 = 1 / sqrt(mean(f^2) + eps)   ((.): per element)
+ *   h  = x' r2 (.) w2                r2 = 1 / sqrt(mean(x'^2) + eps)
+ *
+ *  residual      x: [n_tokens, d_model] of residual_dtype, device, read.
+ *  block         f: [n_tokens, d_model] of dtype, device, read, or NULL: then x' = x, which is not
+ *                written (residual_out, post_weight and gate NULL), and only h is formed.
+ *  post_weight   w1: [d_model] of dtype, device, read, or NULL: f is not normed (r1 = w1 = 1).
+ *  gate          g: [n_tokens, d_model] of dtype with pitch gate_stride, or [d_model] for all rows with
+ *                gate_stride 0, device, read, or NULL: 1.
+ *  pre_weight    w2: [d_model] of dtype, device, read, or NULL: no h (hidden NULL).
+ *  residual_scale s, finite; eps >= 0.
+ *  residual_out  x': of residual_dtype, device, written; may be residual itself.
+ *  hidden        h: of dtype, device, written.  Formed from x' before x' is rounded to residual_dtype.
+ *  Dtypes: residual_dtype f32 with dtype f32 or bf16, or both bf16.  Arithmetic and sums are fp32; what is
+ *  written is rounded to nearest even once.  d_model in [1, 2^20], any; bases and row
+ *  pitches in bytes must be multiples of 16 (GRPO_ERR_ALIGN), pitches at least d_model (GRPO_ERR_SHAPE);
+ *  padding elements are neither read nor written.
+ *  n_tokens == 0 does nothing in the forward.  Outputs may not overlap inputs or one another except as said.
+ * ------------------------------------------------------------------------- */
+grpo_status grpo_block_norm_fwd(const void *residual, int64_t residual_stride, grpo_dtype residual_dtype,
+                                const void *block, int64_t block_stride, const void *post_weight,
+                                const void *gate, int64_t gate_stride, const void *pre_weight,
+                                grpo_dtype dtype, int64_t n_tokens, int64_t d_model,
+                                double residual_scale, double eps, void *residual_out,
+                                int64_t residual_out_stride, void *hidden, int64_t hidden_stride, void *stream);
+
+/*
+ * Its gradients.  Inputs as there, but residual_out is x', as the forward wrote it (not read, and NULL, without
+ * pre_weight), and
+ *  grad_hidden       dL/dh, of dtype, read; NULL without pre_weight.
+ *  grad_residual_out dL/dx' from wherever else x' goes, of residual_dtype, read; may be NULL (zero) with
+ *                    pre_weight.
+ * With y1 = f r1, y2 = x' r2, a = w2 (.) dh, D = dx' + r2 (a - y2 mean(a (.) y2)), t = s g (.) w1 (.) D:
+ *  grad_residual     D: of residual_dtype, written; may be grad_residual_out itself.
+ *  grad_block        r1 (t - y1 mean(t (.) y1)), or t without post_weight: of dtype, written; NULL without block.
+ *  grad_gate         s w1 (.) D (.) y1: [n_tokens, d_model] of dtype with pitch grad_gate_stride, or, with
+ *                    gate_stride 0, its sum over the rows, [d_model] f32; NULL without a gate.
+ *  grad_post_weight  sum over rows of s g (.) D (.) y1: [d_model] f32; NULL without post_weight.
+ *  grad_pre_weight   sum over rows of dh (.) y2: [d_model] f32; NULL without pre_weight.
+ * accumulate_grad_weights != 0: the [d_model] f32 gradients are added to, as in grpo_lmhead_loss_fwd_bwd.
+ * Sums over rows: fp32 over some of the rows, those sums in fp64, in a fixed order: bitwise reproducible.
+ * workspace: device, 256-byte aligned, at least grpo_block_norm_workspace_bytes(n_tokens, d_model) bytes,
+ * contents ignored.  n_tokens == 0 writes zeros into the [d_model] gradients (or adds nothing).
+ */
+size_t grpo_block_norm_workspace_bytes(int64_t n_tokens, int64_t d_model);
+grpo_status grpo_block_norm_bwd(const void *residual_out, int64_t residual_out_stride, grpo_dtype residual_dtype,
+                                const void *block, int64_t block_stride, const void *post_weight,
+                                const void *gate, int64_t gate_stride, const void *pre_weight,
+                                grpo_dtype dtype, int64_t n_tokens, int64_t d_model,
+                                double residual_scale, double eps, const void *grad_hidden,
+                                int64_t grad_hidden_stride, const void *grad_residual_out,
+                                int64_t grad_residual_out_stride, void *grad_residual,
+                                int64_t grad_residual_stride, void *grad_block, int64_t grad_block_stride,
+                                void *grad_gate, int64_t grad_gate_stride, float *grad_post_weight,
+                                float *grad_pre_weight, int accumulate_grad_weights, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------- *
+ * What a trainer does with the gradients, over all tensors of a model at once: their
+ * norm, which section 4.1 clips at 0.1, and one AdamW step,
+ *
+ *   norm = sqrt(sum g^2),  coefficient = norm <= max_norm ? 1 : max_norm / norm
+ *   g' = coefficient g
+ *   m  = beta1 m + (1 - beta1) g'        v = beta2 v + (1 - beta2) g'^2
+ *   p  = p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *
+ * Which tensors there are is said once, in a table that grpo_optim_plan_build writes to
+ * host memory and the caller copies to device memory (256-byte aligned) and keeps there;
+ * both calls then take the grpo_optim_plan and the table's device address.  The table
+ * holds addresses: it is made again when a tensor moves.
+ *
+ * One tensor of n values, all arrays contiguous, in the same order, in device memory, at any address that
+ * their type allows (16-byte boundaries are fastest):
+ *  param         f32 or bf16, read and written; NULL in every tensor of a plan that only
+ *                grpo_grad_norm uses (then master, exp_avg, ... are NULL too).
+ *  master        f32, read and written, or NULL.  With it param is bf16, is not read, and
+ *                is written as the master copy rounded to nearest even.  A bf16 param without one
+ *                is rounded after every step, which loses steps of less than 2^-9 of a value.
+ *  grad          f32 or bf16, read (grpo_lmhead_loss_fwd_bwd writes f32).
+ *  exp_avg       m: f32 (state_bits 32), or e4m3 (state_bits 8) with a scale for every 256 values,
+ *  exp_avg_sq    v: f32, or e4m3 of sqrt(v) with a scale for every 256 values; all zero at the start.
+ *  exp_avg_scale, exp_avg_sq_scale  [ceil(n / 256)] f32, read and written: powers of two, the least (from 2^-126 on)
+ *                under which the largest finite of their values is at most 448; NULL with
+ *                state_bits 32.  What a code stands for is code * scale.  Values are rounded to
+ *                nearest even once, after the step has used them; a positive sqrt(v) becomes at least the smallest
+ *                code, 2^-9, and what is not finite becomes NaN.
+ *  weight_decay  finite.
+ * Arithmetic is fp32, each operation rounded by itself, in the order printed above (sums of the norm: fp64).
+ * NaN and Inf in a gradient reach the value's own parameter and moments, and through the
+ * norm's coefficient all of them; they are never hidden.
+ * ------------------------------------------------------------------------- */
+typedef struct grpo_optim_tensor {
+    void *param;
+    float *master;
+    const void *grad;
+    void *exp_avg;
+    void *exp_avg_sq;
+    float *exp_avg_scale;
+    float *exp_avg_sq_scale;
+    int64_t n;                /* 0 .. 2^40; a tensor of 0 values is ignored, its pointers too */
+    double weight_decay;
+    grpo_dtype param_dtype;
+    grpo_dtype grad_dtype;
+    int32_t state_bits;       /* 32 or 8 */
+    int32_t reserved;
+} grpo_optim_tensor;
+
+typedef struct grpo_optim_plan {
+    int64_t n_tensors;
+    int64_t n_chunks;
+    int32_t has_params;       /* 0: for grpo_grad_norm only */
+    int32_t reserved;
+} grpo_optim_plan;
+
+/* Bytes of the table (a pure host function; 0 for invalid sizes). */
+size_t grpo_optim_plan_bytes(const grpo_optim_tensor *tensors /* host */, int64_t n_tensors);
+
+/*
+ * Checks the tensors and writes table and plan (host only, launches nothing).  Errors: GRPO_ERR_NULL, GRPO_ERR_SHAPE,
+ * GRPO_ERR_DTYPE, GRPO_ERR_ALIGN (an address its type does not allow), GRPO_ERR_PARAM (weight_decay),
+ * GRPO_ERR_WORKSPACE (table_bytes too small, or no host memory to check in), GRPO_ERR_OVERLAP (an array that is written shares memory with
+ * another array).
+ */
+grpo_status grpo_optim_plan_build(const grpo_optim_tensor *tensors /* host */, int64_t n_tensors,
+                                  void *table_out /* host */, size_t table_bytes, grpo_optim_plan *plan_out /* host */);
+
+/*
+ * norm_out [2] f32, device, written: the norm of all gradients, and the coefficient above
+ * (max_norm <= 0: 1).  workspace: device, 256-byte aligned, >= grpo_grad_norm_workspace_bytes() bytes,
+ * contents ignored.  Summed in fp64 in a fixed order: bitwise reproducible.  No tensors: norm 0.
+ */
+size_t grpo_grad_norm_workspace_bytes(void);
+grpo_status grpo_grad_norm(const grpo_optim_plan *plan, const void *table /* device */, double max_norm, float *norm_out,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One step.  step: its number t, from 1 on; or step_device: [1] i64, device, read instead (so that a captured graph can be
+ * replayed: the caller counts it up).  lr: the learning rate; or lr_device: [1] f32, device, read instead.
+ *  clip  NULL, or [2] f32, device, read: what grpo_grad_norm wrote; its coefficient multiplies every gradient.
+ *  beta1, beta2 in [0, 1), eps >= 0.  A number in step_device that is not positive gives NaN or Inf.
+ */
+grpo_status grpo_adamw_step(const grpo_optim_plan *plan, const void *table /* device */, int64_t step, const int64_t *step_device,
+                            double lr, const float *lr_device, double beta1, double beta2, double eps, const float *clip,
+                            void *stream);
 
 #ifdef __cplusplus
 }

@@ -125,6 +125,23 @@ def _load_lib():
     L.grpo_lmhead_loss_aux_fwd_bwd.argtypes = [vp, i64, vp, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp,
                                                f32, f32, f32, f32, f32, f32, f64, f32, vp, vp, vp, vp,
                                                vp, i64, vp, i64, i32, vp, sz, vp]
+    L.grpo_block_norm_fwd.restype = i32
+    L.grpo_block_norm_fwd.argtypes = [vp, i64, i32, vp, i64, vp, vp, i64, vp, i32, i64, i64, f64, f64, vp, i64, vp, i64, vp]
+    L.grpo_block_norm_workspace_bytes.restype = sz
+    L.grpo_block_norm_workspace_bytes.argtypes = [i64, i64]
+    L.grpo_block_norm_bwd.restype = i32
+    L.grpo_block_norm_bwd.argtypes = [vp, i64, i32, vp, i64, vp, vp, i64, vp, i32, i64, i64, f64, f64, vp, i64, vp, i64, vp, i64,
+                                      vp, i64, vp, i64, vp, vp, i32, vp, sz, vp]
+    L.grpo_optim_plan_bytes.restype = sz
+    L.grpo_optim_plan_bytes.argtypes = [ctypes.POINTER(_OptimTensor), i64]
+    L.grpo_optim_plan_build.restype = i32
+    L.grpo_optim_plan_build.argtypes = [ctypes.POINTER(_OptimTensor), i64, vp, sz, ctypes.POINTER(_OptimPlan)]
+    L.grpo_grad_norm_workspace_bytes.restype = sz
+    L.grpo_grad_norm_workspace_bytes.argtypes = []
+    L.grpo_grad_norm.restype = i32
+    L.grpo_grad_norm.argtypes = [ctypes.POINTER(_OptimPlan), vp, f64, vp, vp, sz, vp]
+    L.grpo_adamw_step.restype = i32
+    L.grpo_adamw_step.argtypes = [ctypes.POINTER(_OptimPlan), vp, i64, vp, f64, vp, f64, f64, f64, vp, vp]
     fast = _load_fastcall()
     if fast is not None:
         fast.bind(*[ctypes.cast(f, vp).value for f in (
@@ -147,6 +164,20 @@ def status_string(status) -> str:
 
 def grpo_workspace_bytes(n_tokens: int) -> int:
     return int(lib().grpo_workspace_bytes(int(n_tokens)))
+
+
+class _OptimTensor(ctypes.Structure):
+    """grpo_optim_tensor of grpo.h."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("param", "master", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale",
+                                                     "exp_avg_sq_scale")] + \
+               [("n", ctypes.c_int64), ("weight_decay", ctypes.c_double), ("param_dtype", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class _OptimPlan(ctypes.Structure):
+    """grpo_optim_plan of grpo.h."""
+    _fields_ = [("n_tensors", ctypes.c_int64), ("n_chunks", ctypes.c_int64), ("has_params", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 class RowPlan(ctypes.Structure):
@@ -647,3 +678,250 @@ def grpo_lmhead_loss_aux_fwd_bwd(hidden, weight, tokens, old_logprobs, ref_logpr
     if rc != GRPO_OK:
         raise GrpoError(rc, "grpo_lmhead_loss_aux_fwd_bwd")
     return loss_out, logprobs_out, entropy_out, counts_out, grad_hidden, grad_weight
+
+
+_DTYPE_CODES = {torch.float32: GRPO_F32, torch.bfloat16: GRPO_BF16}
+
+
+def _block_norm_rows(t, name, dtype, n, d, device):
+    """The pitch of an [n, d] tensor whose rows have unit stride."""
+    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != n or t.shape[1] != d or (t.stride(1) != 1 and d > 1):
+        raise ValueError("%s must be a %s tensor [%d, %d] with unit stride along d_model" % (name, dtype, n, d))
+    if t.device != device:
+        raise ValueError("%s must live on %s" % (name, device))
+    return t.stride(0) if n > 1 else max(t.stride(0), d)
+
+
+def _block_norm_args(residual, block, post_weight, gate, pre_weight, dtype):
+    """Device, sizes, dtype and the pitches of the residual stream, the block's output and the gate."""
+    if not residual.is_cuda:
+        raise ValueError("residual must be a device tensor: libgrpo has no CPU path")
+    if residual.dim() != 2 or residual.dtype not in _DTYPE_CODES:
+        raise ValueError("residual must be a float32 or bfloat16 tensor [n_tokens, d_model]")
+    if dtype not in _DTYPE_CODES:
+        raise ValueError("block, gate and weights must be float32 or bfloat16")
+    dev = residual.device
+    n, d = residual.shape
+    rs = _block_norm_rows(residual, "residual", residual.dtype, n, d, dev)
+    fs = gs = 0
+    if block is not None:
+        fs = _block_norm_rows(block, "block", dtype, n, d, dev)
+    if post_weight is not None:
+        _check(post_weight, dtype, d, "post_weight", dev)
+    if pre_weight is not None:
+        _check(pre_weight, dtype, d, "pre_weight", dev)
+    if gate is not None and gate.dim() == 1:
+        _check(gate, dtype, d, "gate", dev)
+    elif gate is not None:
+        gs = _block_norm_rows(gate, "gate", dtype, n, d, dev)
+        if gs == 0 and n > 1:
+            raise ValueError("a gate for all rows is a tensor [d_model]")
+    return dev, n, d, rs, fs, gs
+
+
+def _new_rows(n, d, dtype, device):
+    """[n, d] with rows on 16-byte boundaries."""
+    per16 = 8 if dtype == torch.bfloat16 else 4
+    if d % per16 == 0:
+        return torch.empty((n, d), dtype=dtype, device=device)
+    return torch.empty((n, d + per16 - d % per16), dtype=dtype, device=device)[:, :d]
+
+
+def grpo_block_norm_fwd(residual, block=None, post_weight=None, gate=None, pre_weight=None, residual_scale=1.0, eps=1e-6, *,
+                        residual_out=None, hidden=None, inplace=False, stream=None):
+    """Returns (residual_out, hidden): residual + residual_scale * gate * norm(block) * post_weight, and its norm times
+    pre_weight (None without one); see grpo_block_norm_fwd in grpo.h.  ``gate`` is [n_tokens, d_model], or [d_model] for all
+    rows.  Without a block residual_out is residual itself; ``inplace=True`` writes over it."""
+    dtype = next((t.dtype for t in (block, pre_weight) if t is not None), residual.dtype)
+    dev, n, d, rs, fs, gs = _block_norm_args(residual, block, post_weight, gate, pre_weight, dtype)
+    os_ = hs = 0
+    if block is not None:
+        if inplace:
+            residual_out = residual
+        elif residual_out is None:
+            residual_out = _new_rows(n, d, residual.dtype, dev)
+        os_ = _block_norm_rows(residual_out, "residual_out", residual.dtype, n, d, dev)
+    elif residual_out is not None:
+        raise ValueError("residual_out is written only where there is a block")
+    if pre_weight is not None:
+        if hidden is None:
+            hidden = _new_rows(n, d, dtype, dev)
+        hs = _block_norm_rows(hidden, "hidden", dtype, n, d, dev)
+    elif hidden is not None:
+        raise ValueError("hidden is written only where there is a pre_weight")
+    rc = lib().grpo_block_norm_fwd(_ptr(residual), rs, _DTYPE_CODES[residual.dtype], _ptr(block), fs, _ptr(post_weight), _ptr(gate), gs,
+                                   _ptr(pre_weight), _DTYPE_CODES[dtype], n, d, float(residual_scale), float(eps), _ptr(residual_out),
+                                   os_, _ptr(hidden), hs, _raw_stream(stream, dev.index))
+    if rc != GRPO_OK:
+        raise GrpoError(rc, "grpo_block_norm_fwd")
+    return (residual if block is None else residual_out), hidden
+
+
+def grpo_block_norm_bwd(residual_out, block=None, post_weight=None, gate=None, pre_weight=None, grad_hidden=None,
+                        grad_residual_out=None, residual_scale=1.0, eps=1e-6, *, grad_residual=None, grad_block=None, grad_gate=None,
+                        grad_post_weight=None, grad_pre_weight=None, accumulate_grad_weights=False, workspace=None, stream=None):
+    """Gradients of grpo_block_norm_fwd, whose residual_out this takes; see grpo_block_norm_bwd in grpo.h.
+
+    Returns (grad_residual, grad_block, grad_gate, grad_post_weight, grad_pre_weight), None for what there is not.  The
+    gradients of the weights, and of a gate for all rows, are f32 [d_model]."""
+    dtype = next((t.dtype for t in (block, pre_weight) if t is not None), residual_out.dtype)
+    dev, n, d, rs, fs, gs = _block_norm_args(residual_out, block, post_weight, gate, pre_weight, dtype)
+    if (grad_hidden is None) != (pre_weight is None):
+        raise ValueError("grad_hidden goes with pre_weight")
+    hs = 0 if grad_hidden is None else _block_norm_rows(grad_hidden, "grad_hidden", dtype, n, d, dev)
+    os_ = 0 if grad_residual_out is None else _block_norm_rows(grad_residual_out, "grad_residual_out", residual_out.dtype, n, d, dev)
+    if grad_residual is None:
+        grad_residual = _new_rows(n, d, residual_out.dtype, dev)
+    dxs = _block_norm_rows(grad_residual, "grad_residual", residual_out.dtype, n, d, dev)
+    dfs = dgs = 0
+    if block is not None:
+        if grad_block is None:
+            grad_block = _new_rows(n, d, dtype, dev)
+        dfs = _block_norm_rows(grad_block, "grad_block", dtype, n, d, dev)
+    sums = [(grad_post_weight, post_weight, "grad_post_weight"), (grad_pre_weight, pre_weight, "grad_pre_weight")]
+    if gate is not None and gate.dim() == 1:
+        sums.append((grad_gate, gate, "grad_gate"))
+    elif gate is not None:
+        if grad_gate is None:
+            grad_gate = _new_rows(n, d, dtype, dev)
+        dgs = _block_norm_rows(grad_gate, "grad_gate", dtype, n, d, dev)
+    made = []
+    for grad, of, name in sums:
+        if of is not None and grad is None:
+            if accumulate_grad_weights:
+                raise ValueError("accumulate_grad_weights needs the %s tensor to add to" % name)
+            grad = torch.empty(d, dtype=torch.float32, device=dev)
+        elif grad is not None:
+            _check(grad, torch.float32, d, name, dev)
+        made.append(grad)
+    grad_post_weight, grad_pre_weight = made[:2]
+    if len(made) > 2:
+        grad_gate = made[2]
+    L = lib()
+    if workspace is None:
+        workspace = torch.empty(L.grpo_block_norm_workspace_bytes(n, d), dtype=torch.uint8, device=dev)
+    rc = L.grpo_block_norm_bwd(_ptr(residual_out) if pre_weight is not None else None, rs, _DTYPE_CODES[residual_out.dtype], _ptr(block), fs,
+                               _ptr(post_weight), _ptr(gate), gs, _ptr(pre_weight), _DTYPE_CODES[dtype], n, d, float(residual_scale),
+                               float(eps), _ptr(grad_hidden), hs, _ptr(grad_residual_out), os_, _ptr(grad_residual), dxs, _ptr(grad_block),
+                               dfs, _ptr(grad_gate), dgs, _ptr(grad_post_weight), _ptr(grad_pre_weight),
+                               1 if accumulate_grad_weights else 0, _ptr(workspace), workspace.numel(), _raw_stream(stream, dev.index))
+    if rc != GRPO_OK:
+        raise GrpoError(rc, "grpo_block_norm_bwd")
+    return grad_residual, grad_block, grad_gate, grad_post_weight, grad_pre_weight
+
+
+class OptimPlan:
+    """The tensors of a model as grpo_grad_norm and grpo_adamw_step take them: made by grpo_optim_plan, which see.  It
+    keeps the tensors it was made from alive."""
+
+    def __init__(self, plan, table, tensors):
+        self._plan, self._table, self._tensors = plan, table, tensors
+        self._by_ref = ctypes.byref(plan)
+
+    @property
+    def device(self):
+        return self._table.device
+
+
+def _optim_list(tensors, n, name, dtypes, device):
+    """`tensors` as a list of n contiguous tensors of one of the dtypes on the device; n times None where there are none."""
+    if tensors is None:
+        return [None] * n
+    tensors = list(tensors)
+    if len(tensors) != n:
+        raise ValueError("%s has %d tensors and grads %d" % (name, len(tensors), n))
+    for t in tensors:
+        if t is not None and (t.dtype not in dtypes or not t.is_contiguous() or t.device != device):
+            raise ValueError("%s must be contiguous tensors of %s on %s" % (name, " or ".join(str(d) for d in dtypes), device))
+    return tensors
+
+
+def grpo_optim_plan(params, grads, exp_avgs=None, exp_avg_sqs=None, *, masters=None, exp_avg_scales=None, exp_avg_sq_scales=None,
+                    weight_decay=0.0):
+    """An OptimPlan of these tensors; see grpo_optim_tensor and grpo_optim_plan_build in grpo.h.
+
+    Lists of equal length, a tensor's gradient, moments, ... at its own place: params f32 or bf16 (None: the plan is for
+    grpo_grad_norm only), grads f32 or bf16, exp_avgs and exp_avg_sqs f32, or float8_e4m3fn with exp_avg_scales and
+    exp_avg_sq_scales, one f32 for every 256 values; masters f32 or None, as a whole or in single places.  weight_decay: a
+    number, or a list of them.  The plan holds the tensors' addresses: gradients are brought into the same tensors before
+    every step, and moments and parameters are changed in them."""
+    grads = list(grads)
+    n = len(grads)
+    if not grads:
+        raise ValueError("there are no tensors")
+    dev = grads[0].device
+    if dev.type != "cuda":
+        raise ValueError("grads must be device tensors: libgrpo has no CPU path")
+    f32, bf16, e4m3 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+    grads = _optim_list(grads, n, "grads", (f32, bf16), dev)
+    params = _optim_list(params, n, "params", (f32, bf16), dev)
+    masters = _optim_list(masters, n, "masters", (f32,), dev)
+    m = _optim_list(exp_avgs, n, "exp_avgs", (f32, e4m3), dev)
+    v = _optim_list(exp_avg_sqs, n, "exp_avg_sqs", (f32, e4m3), dev)
+    ms = _optim_list(exp_avg_scales, n, "exp_avg_scales", (f32,), dev)
+    vs = _optim_list(exp_avg_sq_scales, n, "exp_avg_sq_scales", (f32,), dev)
+    decay = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+    if len(decay) != n:
+        raise ValueError("weight_decay has %d numbers and grads %d tensors" % (len(decay), n))
+    table = (_OptimTensor * n)()
+    for i, e in enumerate(table):
+        count = grads[i].numel()
+        for t, name in ((params[i], "param"), (masters[i], "master"), (m[i], "exp_avg"), (v[i], "exp_avg_sq")):
+            if t is not None and t.numel() != count:
+                raise ValueError("tensor %d: %s has %d values and its gradient %d" % (i, name, t.numel(), count))
+        if m[i] is not None and v[i] is not None and m[i].dtype != v[i].dtype:
+            raise ValueError("tensor %d: both moments must be of the same dtype" % i)
+        for t, name in ((ms[i], "exp_avg_scale"), (vs[i], "exp_avg_sq_scale")):
+            if t is not None and t.numel() != (count + 255) // 256:
+                raise ValueError("tensor %d: %s must have one value for every 256" % (i, name))
+        e.param, e.master, e.grad, e.exp_avg, e.exp_avg_sq = (_ptr(t) for t in (params[i], masters[i], grads[i], m[i], v[i]))
+        e.exp_avg_scale, e.exp_avg_sq_scale = _ptr(ms[i]), _ptr(vs[i])
+        e.n, e.weight_decay = count, decay[i]
+        e.param_dtype = GRPO_BF16 if params[i] is not None and params[i].dtype == bf16 else GRPO_F32
+        e.grad_dtype = GRPO_BF16 if grads[i].dtype == bf16 else GRPO_F32
+        e.state_bits = 8 if m[i] is not None and m[i].dtype == e4m3 else 32
+    host = torch.empty(int(lib().grpo_optim_plan_bytes(table, n)), dtype=torch.uint8)
+    plan = _OptimPlan()
+    rc = lib().grpo_optim_plan_build(table, n, _ptr(host), host.numel(), ctypes.byref(plan))
+    if rc != GRPO_OK:
+        raise GrpoError(rc, "grpo_optim_plan_build")
+    return OptimPlan(plan, host.to(dev), [t for group in (params, masters, grads, m, v, ms, vs) for t in group if t is not None])
+
+
+def grpo_grad_norm(plan, max_norm=0.0, *, norm_out=None, workspace=None, stream=None):
+    """[2] f32: the norm of all the plan's gradients, and the coefficient that clips it at max_norm (1 where there is none);
+    see grpo_grad_norm in grpo.h."""
+    dev = plan.device
+    if norm_out is None:
+        norm_out = torch.empty(2, dtype=torch.float32, device=dev)
+    else:
+        _check(norm_out, torch.float32, 2, "norm_out", dev)
+    L = lib()
+    if workspace is None:
+        workspace = torch.empty(L.grpo_grad_norm_workspace_bytes(), dtype=torch.uint8, device=dev)
+    rc = L.grpo_grad_norm(plan._by_ref, _ptr(plan._table), float(max_norm), _ptr(norm_out), _ptr(workspace), workspace.numel(),
+                          _raw_stream(stream, dev.index))
+    if rc != GRPO_OK:
+        raise GrpoError(rc, "grpo_grad_norm")
+    return norm_out
+
+
+def grpo_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, *, clip=None, stream=None):
+    """One AdamW step over the plan's tensors, in place; see grpo_adamw_step in grpo.h.
+
+    ``step`` counts from 1; ``step`` (i64) and ``lr`` (f32) may be device tensors of one value, which a captured graph reads at
+    every replay.  ``clip``: what grpo_grad_norm returned."""
+    dev = plan.device
+    step_at = lr_at = None
+    if isinstance(step, torch.Tensor):
+        _check(step, torch.int64, 1, "step", dev)
+        step, step_at = 0, _ptr(step)
+    if isinstance(lr, torch.Tensor):
+        _check(lr, torch.float32, 1, "lr", dev)
+        lr, lr_at = 0.0, _ptr(lr)
+    if clip is not None:
+        _check(clip, torch.float32, 2, "clip", dev)
+    rc = lib().grpo_adamw_step(plan._by_ref, _ptr(plan._table), int(step), step_at, float(lr), lr_at, float(beta1), float(beta2),
+                               float(eps), _ptr(clip), _raw_stream(stream, dev.index))
+    if rc != GRPO_OK:
+        raise GrpoError(rc, "grpo_adamw_step")

@@ -1,0 +1,403 @@
+// The norms around a block of the model, with the block's gate and the scale it is added to the residual stream with, and
+// their gradients.  Part of grpo.hip's translation unit.
+//
+//   x' = x + s g (.) f r1 (.) w1      r1 = 1 / sqrt(mean(f^2) + eps)      f: the block's output, x: the residual stream
+//   h  = x' r2 (.) w2                 r2 = 1 / sqrt(mean(x'^2) + eps)     h: what the next block, or the head, takes
+//
+// and with y2 = x' r2, a = w2 (.) dh, y1 = f r1:
+//
+//   dx  = D = dx' + r2 (a - y2 mean(a (.) y2))          dw2 = sum over rows of dh (.) y2
+//   t   = s g (.) w1 (.) D                              dw1 = sum over rows of s g (.) D (.) y1
+//   df  = r1 (t - y1 mean(t (.) y1))                    dg  = s w1 (.) D (.) y1 (summed over rows where one gate serves all)
+//
+// Both norms' 1/sqrt are formed again in the backward: their sums go along with those it needs anyway.
+
+namespace __attribute__((visibility("hidden"))) grpo_impl {
+
+struct BlockNorm {
+    const char *x, *f, *w1, *g, *w2, *dh, *dxo;  // forward: x = the residual stream; backward: x = x'
+    char *xo, *h;                                // forward
+    char *dx, *df, *dg;                          // backward; dg here where every row has a gate
+    float *part;                                 // backward: [grid][2][d] sums over a workgroup's rows
+    long long xs, fs, gs, dhs, dxos, xos, hs, dxs, dfs, dgs;  // row pitches in bytes
+    long long n;
+    int d;
+    float scale, eps, inv_d;
+};
+
+// VEC neighbours of a row, in fp32; zeros behind its end.
+template <grpo_dtype DT, int VEC>
+__device__ __forceinline__ void row_load(const char *row, int col, int d, float (&v)[VEC])
+{
+    constexpr int B = Elem<DT>::BYTES;
+    if (col + VEC <= d) {
+        if constexpr (VEC * B == 16) {
+            unpack<DT>(*(const u32x4 *)(row + (size_t)col * B), v);
+        } else {
+            static_assert(DT == GRPO_BF16 && VEC == 4, "four bf16 values beside four fp32 ones");
+            const u32x2 u = *(const u32x2 *)(row + (size_t)col * B);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                v[2 * i] = as_f32(u[i] << 16);
+                v[2 * i + 1] = as_f32(u[i] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = col + i < d ? load_elem<DT>(row, col + i) : 0.f;
+    }
+}
+template <grpo_dtype DT, int VEC>
+__device__ __forceinline__ void row_store(char *row, int col, int d, const float (&v)[VEC])
+{
+    constexpr int B = Elem<DT>::BYTES;
+    if (col + VEC <= d) {
+        if constexpr (VEC * B == 16) {
+            *(u32x4 *)(row + (size_t)col * B) = pack<DT>(v);
+        } else {
+            const u32x2 u = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+            *(u32x2 *)(row + (size_t)col * B) = u;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (col + i < d) store_elem<DT>(row, col + i, v[i]);
+    }
+}
+
+constexpr int kNormBlock = 256;
+constexpr long long kNormGrid = 1024;  // workgroups of the backward at most, each with a row of partial sums
+
+// What is added to the residual stream, without the scale: the block's output, normed, weighted and gated.
+template <grpo_dtype DT, int VEC>
+__device__ __forceinline__ void branch(const BlockNorm &p, const char *g, int col, float r1, float (&f)[VEC])
+{
+    float w[VEC];
+    if (p.w1) {
+        row_load<DT, VEC>(p.w1, col, p.d, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[i] *= r1 * w[i];
+    }
+    if (g) {
+        row_load<DT, VEC>(g, col, p.d, w);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[i] *= w[i];
+    }
+}
+
+template <grpo_dtype RT, grpo_dtype DT>
+__global__ void __launch_bounds__(kNormBlock) block_norm_fwd_k(BlockNorm p)
+{
+    constexpr int VEC = 16 / Elem<RT>::BYTES;
+    __shared__ float lds[2][kNormBlock / 64];
+    for (long long row = blockIdx.x; row < p.n; row += gridDim.x) {
+        const char *x = p.x + row * p.xs, *f = p.f ? p.f + row * p.fs : nullptr, *g = p.g ? p.g + row * p.gs : nullptr;
+        float r1 = 1.f, r2 = 0.f, sum = 0.f;
+        if (p.w1) {
+            for (int col = threadIdx.x * VEC; col < p.d; col += kNormBlock * VEC) {
+                float v[VEC];
+                row_load<DT, VEC>(f, col, p.d, v);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum += v[i] * v[i];
+            }
+            r1 = 1.f / sqrtf(block_sum<kNormBlock>(sum, lds[0]) * p.inv_d + p.eps);
+        }
+        sum = 0.f;
+        for (int pass = p.w2 ? 0 : 1; pass < 2; ++pass) {
+            for (int col = threadIdx.x * VEC; col < p.d; col += kNormBlock * VEC) {
+                float v[VEC], b[VEC];
+                row_load<RT, VEC>(x, col, p.d, v);
+                if (f) {
+                    row_load<DT, VEC>(f, col, p.d, b);
+                    branch<DT, VEC>(p, g, col, r1, b);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) v[i] += p.scale * b[i];
+                }
+                if (pass == 0) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) sum += v[i] * v[i];
+                    continue;
+                }
+                if (f) row_store<RT, VEC>(p.xo + row * p.xos, col, p.d, v);
+                if (p.w2) {
+                    row_load<DT, VEC>(p.w2, col, p.d, b);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) v[i] *= r2 * b[i];
+                    row_store<DT, VEC>(p.h + row * p.hs, col, p.d, v);
+                }
+            }
+            if (pass == 0) r2 = 1.f / sqrtf(block_sum<kNormBlock>(sum, lds[1]) * p.inv_d + p.eps);
+        }
+        __syncthreads();  // the next row's sums go where this one's were
+    }
+}
+
+template <grpo_dtype RT, grpo_dtype DT>
+__global__ void __launch_bounds__(kNormBlock) block_norm_bwd_k(BlockNorm p)
+{
+    constexpr int VEC = 16 / Elem<RT>::BYTES;
+    __shared__ float lds[4][kNormBlock / 64];
+    float *part = p.part + (size_t)blockIdx.x * 2 * p.d;
+    for (long long row = blockIdx.x; row < p.n; row += gridDim.x) {
+        const char *x = p.x + row * p.xs, *f = p.f ? p.f + row * p.fs : nullptr, *g = p.g ? p.g + row * p.gs : nullptr;
+        const char *dh = p.w2 ? p.dh + row * p.dhs : nullptr, *dxo = p.dxo ? p.dxo + row * p.dxos : nullptr;
+        float sx = 0.f, sax = 0.f, sf = 0.f;
+        for (int col = threadIdx.x * VEC; col < p.d; col += kNormBlock * VEC) {
+            float v[VEC], w[VEC], u[VEC];
+            if (p.w2) {
+                row_load<RT, VEC>(x, col, p.d, v);
+                row_load<DT, VEC>(dh, col, p.d, u);
+                row_load<DT, VEC>(p.w2, col, p.d, w);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    sx += v[i] * v[i];
+                    sax += u[i] * w[i] * v[i];
+                }
+            }
+            if (p.w1) {
+                row_load<DT, VEC>(f, col, p.d, v);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sf += v[i] * v[i];
+            }
+        }
+        block_sum2<kNormBlock>(sx, sax, lds[0], lds[1]);
+        const float r1 = p.w1 ? 1.f / sqrtf(block_sum<kNormBlock>(sf, lds[2]) * p.inv_d + p.eps) : 1.f;
+        const float r2 = 1.f / sqrtf(sx * p.inv_d + p.eps);
+        const float c2 = sax * r2 * p.inv_d;  // mean(a y2)
+        float sty = 0.f, c1 = 0.f;
+        for (int pass = p.w1 ? 0 : 1; pass < 2; ++pass) {
+            for (int col = threadIdx.x * VEC; col < p.d; col += kNormBlock * VEC) {
+                float v[VEC], w[VEC], u[VEC], D[VEC] = {};
+                if (dxo) row_load<RT, VEC>(dxo, col, p.d, D);
+                if (p.w2) {
+                    row_load<RT, VEC>(x, col, p.d, v);
+                    row_load<DT, VEC>(dh, col, p.d, u);
+                    row_load<DT, VEC>(p.w2, col, p.d, w);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        const float y2 = v[i] * r2;
+                        D[i] += r2 * (u[i] * w[i] - y2 * c2);
+                        v[i] = u[i] * y2;  // its share of dw2
+                    }
+                    if (pass == 1)
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i)
+                            if (col + i < p.d) part[col + i] = (row == blockIdx.x ? 0.f : part[col + i]) + v[i];
+                }
+                if (pass == 1) row_store<RT, VEC>(p.dx + row * p.dxs, col, p.d, D);
+                if (!f) continue;
+                float y[VEC], gate[VEC], w1[VEC], t[VEC], sum[VEC];
+                row_load<DT, VEC>(f, col, p.d, y);
+                if (p.w1) row_load<DT, VEC>(p.w1, col, p.d, w1);
+                if (g) row_load<DT, VEC>(g, col, p.d, gate);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    y[i] *= r1;
+                    if (!p.w1) w1[i] = 1.f;
+                    if (!g) gate[i] = 1.f;
+                    const float sD = p.scale * D[i];
+                    t[i] = sD * gate[i] * w1[i];
+                    sum[i] = sD * y[i] * (p.gs ? gate[i] : 1.f);
+                    gate[i] = sD * y[i] * w1[i];  // its gradient
+                    if (pass == 0) sty += t[i] * y[i];
+                }
+                if (pass == 0) continue;
+                if (p.w1) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) t[i] = r1 * (t[i] - y[i] * c1);
+                }
+                row_store<DT, VEC>(p.df + row * p.dfs, col, p.d, t);
+                if (p.dg) row_store<DT, VEC>(p.dg + row * p.dgs, col, p.d, gate);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    if (col + i < p.d) part[p.d + col + i] = (row == blockIdx.x ? 0.f : part[p.d + col + i]) + sum[i];
+            }
+            if (pass == 0) c1 = block_sum<kNormBlock>(sty, lds[3]) * p.inv_d;
+        }
+        __syncthreads();
+    }
+}
+
+// The workgroups' sums, added up in fp64 in their order.  With one gate for all rows (or none) the second sum is that of
+// s D (.) y1, which gives both dw1, times the gate, and the gate's gradient, times w1.
+template <grpo_dtype DT>
+__global__ void __launch_bounds__(256) block_norm_columns(const float *part, int blocks, int d, const char *w1, const char *gate_row,
+                                                          float *dw1, float *dgate_row, float *dw2, int accumulate)
+{
+    const int col = blockIdx.x * 256 + threadIdx.x;
+    if (col >= d) return;
+    if (dw2) {
+        double s = 0.0;
+        for (int b = 0; b < blocks; ++b) s += part[(size_t)b * 2 * d + col];
+        dw2[col] = accumulate ? dw2[col] + (float)s : (float)s;
+    }
+    if (dw1 || dgate_row) {
+        double s = 0.0;
+        for (int b = 0; b < blocks; ++b) s += part[(size_t)b * 2 * d + d + col];
+        if (dw1) {
+            const float v = (float)s * (gate_row ? load_elem<DT>(gate_row, col) : 1.f);
+            dw1[col] = accumulate ? dw1[col] + v : v;
+        }
+        if (dgate_row) {
+            const float v = (float)s * (w1 ? load_elem<DT>(w1, col) : 1.f);
+            dgate_row[col] = accumulate ? dgate_row[col] + v : v;
+        }
+    }
+}
+
+constexpr int64_t kNormMaxWidth = 1 << 20;
+
+// A [n, d] array: present, on 16-byte boundaries, rows at least d apart.
+static grpo_status check_rows(const void *p, int64_t stride, int64_t d, int dtype, bool wanted)
+{
+    if ((p != nullptr) != wanted) return GRPO_ERR_NULL;
+    if (!p) return GRPO_OK;
+    if (stride < d) return GRPO_ERR_SHAPE;
+    const int64_t bytes = dtype == GRPO_BF16 ? 2 : 4;
+    if (((uintptr_t)p & 15u) || ((stride * bytes) & 15)) return GRPO_ERR_ALIGN;
+    return GRPO_OK;
+}
+
+static grpo_status check_block_norm(int rt, int dt, const void *block, const void *w1, const void *gate, int64_t gate_stride, const void *w2,
+                                    int64_t n, int64_t d, double scale, double eps)
+{
+    if ((rt != GRPO_F32 && rt != GRPO_BF16) || (dt != GRPO_F32 && dt != GRPO_BF16) || (rt == GRPO_BF16 && dt == GRPO_F32)) return GRPO_ERR_DTYPE;
+    if (n < 0 || d <= 0 || d > kNormMaxWidth || gate_stride < 0) return GRPO_ERR_SHAPE;
+    if (!std::isfinite(scale) || !(eps >= 0.0) || !std::isfinite(eps)) return GRPO_ERR_PARAM;
+    if (n > 0 && !block && (w1 || gate || !w2)) return GRPO_ERR_NULL;
+    if (gate && gate_stride != 0 && gate_stride < d) return GRPO_ERR_SHAPE;
+    if (((uintptr_t)w1 | (uintptr_t)w2 | (uintptr_t)gate) & 15u) return GRPO_ERR_ALIGN;
+    if (gate && ((gate_stride * (dt == GRPO_BF16 ? 2 : 4)) & 15)) return GRPO_ERR_ALIGN;
+    return GRPO_OK;
+}
+
+static BlockNorm block_norm_params(int rt, int dt, const void *x, int64_t xs, const void *block, int64_t fs, const void *w1, const void *gate,
+                                   int64_t gs, const void *w2, int64_t n, int64_t d, double scale, double eps)
+{
+    const int64_t rb = rt == GRPO_BF16 ? 2 : 4, db = dt == GRPO_BF16 ? 2 : 4;
+    BlockNorm p = {};
+    p.x = (const char *)x;
+    p.xs = xs * rb;
+    p.f = (const char *)block;
+    p.fs = fs * db;
+    p.w1 = (const char *)w1;
+    p.g = (const char *)gate;
+    p.gs = gs * db;
+    p.w2 = (const char *)w2;
+    p.n = n;
+    p.d = (int)d;
+    p.scale = (float)scale;
+    p.eps = (float)eps;
+    p.inv_d = (float)(1.0 / (double)d);
+    return p;
+}
+
+template <grpo_dtype RT, grpo_dtype DT>
+static void launch_block_norm_fwd(const BlockNorm &p, hipStream_t st)
+{
+    const long long grid = p.n < 65536 ? p.n : 65536;
+    hipLaunchKernelGGL((block_norm_fwd_k<RT, DT>), dim3((unsigned)grid), dim3(kNormBlock), 0, st, p);
+}
+
+template <grpo_dtype RT, grpo_dtype DT>
+static void launch_block_norm_bwd(const BlockNorm &p, hipStream_t st, float *dw1, float *dgate_row, float *dw2, int accumulate)
+{
+    const long long grid = p.n < kNormGrid ? p.n : kNormGrid;
+    if (p.n > 0) hipLaunchKernelGGL((block_norm_bwd_k<RT, DT>), dim3((unsigned)grid), dim3(kNormBlock), 0, st, p);
+    hipLaunchKernelGGL((block_norm_columns<DT>), dim3((unsigned)((p.d + 255) / 256)), dim3(256), 0, st, p.part, (int)grid, p.d, p.w1,
+                       p.gs ? nullptr : p.g, dw1, dgate_row, dw2, accumulate);
+}
+
+}  // namespace grpo_impl
+
+extern "C" {
+
+grpo_status grpo_block_norm_fwd(const void *residual, int64_t residual_stride, grpo_dtype residual_dtype, const void *block,
+                                int64_t block_stride, const void *post_weight, const void *gate, int64_t gate_stride,
+                                const void *pre_weight, grpo_dtype dtype, int64_t n_tokens, int64_t d_model, double residual_scale,
+                                double eps, void *residual_out, int64_t residual_out_stride, void *hidden, int64_t hidden_stride, void *stream)
+{
+    const int rt = raw_enum(residual_dtype), dt = raw_enum(dtype);
+    grpo_status bad = check_block_norm(rt, dt, block, post_weight, gate, gate_stride, pre_weight, n_tokens, d_model, residual_scale, eps);
+    if (bad != GRPO_OK) return bad;
+    if (n_tokens == 0) return GRPO_OK;
+    if ((bad = check_rows(residual, residual_stride, d_model, rt, true)) != GRPO_OK) return bad;
+    if ((bad = check_rows(block, block_stride, d_model, dt, block != nullptr)) != GRPO_OK) return bad;
+    if ((bad = check_rows(residual_out, residual_out_stride, d_model, rt, block != nullptr)) != GRPO_OK) return bad;
+    if ((bad = check_rows(hidden, hidden_stride, d_model, dt, pre_weight != nullptr)) != GRPO_OK) return bad;
+    BlockNorm p = block_norm_params(rt, dt, residual, residual_stride, block, block_stride, post_weight, gate, gate_stride, pre_weight,
+                                    n_tokens, d_model, residual_scale, eps);
+    p.xo = (char *)residual_out;
+    p.xos = residual_out_stride * (rt == GRPO_BF16 ? 2 : 4);
+    p.h = (char *)hidden;
+    p.hs = hidden_stride * (dt == GRPO_BF16 ? 2 : 4);
+    hipStream_t st = (hipStream_t)stream;
+    if (rt == GRPO_BF16)
+        launch_block_norm_fwd<GRPO_BF16, GRPO_BF16>(p, st);
+    else if (dt == GRPO_BF16)
+        launch_block_norm_fwd<GRPO_F32, GRPO_BF16>(p, st);
+    else
+        launch_block_norm_fwd<GRPO_F32, GRPO_F32>(p, st);
+    return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
+}
+
+size_t grpo_block_norm_workspace_bytes(int64_t n_tokens, int64_t d_model)
+{
+    if (n_tokens < 0 || d_model <= 0 || d_model > kNormMaxWidth) return 0;
+    const size_t blocks = (size_t)(n_tokens < kNormGrid ? n_tokens : kNormGrid);
+    return align_up(blocks * 2 * (size_t)d_model * 4 + 1, 256);
+}
+
+grpo_status grpo_block_norm_bwd(const void *residual_out, int64_t residual_out_stride, grpo_dtype residual_dtype, const void *block,
+                                int64_t block_stride, const void *post_weight, const void *gate, int64_t gate_stride,
+                                const void *pre_weight, grpo_dtype dtype, int64_t n_tokens, int64_t d_model, double residual_scale,
+                                double eps, const void *grad_hidden, int64_t grad_hidden_stride, const void *grad_residual_out,
+                                int64_t grad_residual_out_stride, void *grad_residual, int64_t grad_residual_stride, void *grad_block,
+                                int64_t grad_block_stride, void *grad_gate, int64_t grad_gate_stride, float *grad_post_weight,
+                                float *grad_pre_weight, int accumulate_grad_weights, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int rt = raw_enum(residual_dtype), dt = raw_enum(dtype);
+    grpo_status bad = check_block_norm(rt, dt, block, post_weight, gate, gate_stride, pre_weight, n_tokens, d_model, residual_scale, eps);
+    if (bad != GRPO_OK) return bad;
+    if ((post_weight != nullptr) != (grad_post_weight != nullptr) || (pre_weight != nullptr) != (grad_pre_weight != nullptr)) return GRPO_ERR_NULL;
+    const bool gates = gate && gate_stride != 0;  // one for every row
+    if (gate && !gates && !grad_gate) return GRPO_ERR_NULL;
+    if (n_tokens > 0) {
+        if ((bad = check_rows(residual_out, residual_out_stride, d_model, rt, pre_weight != nullptr)) != GRPO_OK) return bad;
+        if ((bad = check_rows(block, block_stride, d_model, dt, block != nullptr)) != GRPO_OK) return bad;
+        if ((bad = check_rows(grad_hidden, grad_hidden_stride, d_model, dt, pre_weight != nullptr)) != GRPO_OK) return bad;
+        if ((bad = check_rows(grad_residual_out, grad_residual_out_stride, d_model, rt, grad_residual_out || !pre_weight)) != GRPO_OK)
+            return bad;
+        if ((bad = check_rows(grad_residual, grad_residual_stride, d_model, rt, true)) != GRPO_OK) return bad;
+        if ((bad = check_rows(grad_block, grad_block_stride, d_model, dt, block != nullptr)) != GRPO_OK) return bad;
+        if (gates || !gate)
+            if ((bad = check_rows(grad_gate, grad_gate_stride, d_model, dt, gates)) != GRPO_OK) return bad;
+    }
+    if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < grpo_block_norm_workspace_bytes(n_tokens, d_model))
+        return GRPO_ERR_WORKSPACE;
+    BlockNorm p = block_norm_params(rt, dt, residual_out, residual_out_stride, block, block_stride, post_weight, gate, gate_stride, pre_weight,
+                                    n_tokens, d_model, residual_scale, eps);
+    const int64_t rb = rt == GRPO_BF16 ? 2 : 4, db = dt == GRPO_BF16 ? 2 : 4;
+    p.dh = (const char *)grad_hidden;
+    p.dhs = grad_hidden_stride * db;
+    p.dxo = (const char *)grad_residual_out;
+    p.dxos = grad_residual_out_stride * rb;
+    p.dx = (char *)grad_residual;
+    p.dxs = grad_residual_stride * rb;
+    p.df = (char *)grad_block;
+    p.dfs = grad_block_stride * db;
+    p.dg = gates ? (char *)grad_gate : nullptr;
+    p.dgs = grad_gate_stride * db;
+    p.part = (float *)workspace;
+    float *gate_row = gate && !gates ? (float *)grad_gate : nullptr;
+    hipStream_t st = (hipStream_t)stream;
+    if (rt == GRPO_BF16)
+        launch_block_norm_bwd<GRPO_BF16, GRPO_BF16>(p, st, grad_post_weight, gate_row, grad_pre_weight, accumulate_grad_weights);
+    else if (dt == GRPO_BF16)
+        launch_block_norm_bwd<GRPO_F32, GRPO_BF16>(p, st, grad_post_weight, gate_row, grad_pre_weight, accumulate_grad_weights);
+    else
+        launch_block_norm_bwd<GRPO_F32, GRPO_F32>(p, st, grad_post_weight, gate_row, grad_pre_weight, accumulate_grad_weights);
+    return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
+}
+
+}  // extern "C"

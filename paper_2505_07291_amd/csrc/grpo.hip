@@ -12,9 +12,13 @@
 // traffic per row instead of 2 reads + 1 write.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <cstring>
+#include <memory>
+#include <new>
 
 #include "grpo.h"
 
@@ -2809,11 +2813,12 @@ const char *grpo_status_string(grpo_status status)
         case GRPO_ERR_ALIGN: return "logits/grad base pointer or row pitch is not 16-byte aligned";
         case GRPO_ERR_PARAM:
             return "bad parameter: need temperature > 0, 0 <= eps_low <= 1, eps_high >= 0, "
-                   "delta > 1 + eps_high, eps_std >= 0, ddof in {0,1}";
+                   "delta > 1 + eps_high, eps_std >= 0, ddof in {0,1}; AdamW: 0 <= beta < 1, eps >= 0, step >= 1, finite rates";
         case GRPO_ERR_WORKSPACE: return "workspace is NULL, not 256-byte aligned or too small";
         case GRPO_ERR_HIP: return "HIP runtime error at kernel launch";
         case GRPO_ERR_CAPACITY:
             return "n_tokens exceeds GRPO_NOALLOC_MAX_TOKENS, the rows the library's built-in scratch array holds";
+        case GRPO_ERR_OVERLAP: return "arrays that must be apart share memory";
     }
     return "unknown status";
 }
@@ -3078,4 +3083,6 @@ grpo_status grpo_workspace_error(const void *workspace, int32_t *flag_out, void 
 }  // extern "C"
 
 #include "lmhead.hpp"
+#include "optim.hpp"
+#include "blocknorm.hpp"
 #endif  // GRPO_ROWS_OF
