@@ -465,6 +465,47 @@ grpo_status grpo_lmhead_loss_aux_fwd_bwd(const void *hidden, int64_t hidden_stri
                                          void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------- *
+ * Tokens of running responses: drafted ones are verified against the target's
+ * probabilities, and one more is sampled, from random numbers that the caller gives.  The
+ * tokens are distributed as if each had been sampled from the target, whatever the drafts.
+ * With drafts == 0 it samples one token for each response.  The log-probs are
+ * those that grpo_loss_fwd_bwd takes as old_logprobs.
+ *
+ * Response b has k = min(draft_lengths[b], drafts) drafted tokens y_0 .. y_{k-1} and target rows 0 .. k: row i is the
+ * target's logits behind y_{i-1}.  With p_i = softmax(target_logits[b, i] / temperature) and
+ * q_i = softmax(draft_logits[b, i] / draft_temperature):
+ *   y_i is accepted iff  accept_u[b, i] q_i(y_i) < p_i(y_i);
+ *   n = the first i < k that is not accepted, or k where all are;
+ *   t = the smallest j with sum_{l <= j} w_l > sample_u[b] sum_l w_l, where w = max(p_n - q_n, 0) if n < k and
+ *       w = p_n if n = k, or if p_n - q_n has nothing above 0.
+ *  target_logits [batch, drafts + 1, vocab] of dtype, device, read; response b's row i starts
+ *                b * target_batch_stride + i * target_row_stride elements behind the first.  Base and
+ *                both strides in bytes must be multiples of 16; target_row_stride >= vocab.  Rows behind k are not read.
+ *  draft_logits  [batch, drafts, vocab] of dtype, likewise; or NULL: q_i has all of its mass on y_i (tokens that no model drafted).
+ *  draft_tokens  [batch, drafts] i64, device, read.  One outside [0, vocab) is not accepted (p_i and q_i are 0 there).
+ *  accept_u      [batch, drafts] f32, sample_u [batch] f64, device, read: uniform in [0, 1).
+ *  draft_lengths [batch] i32, device, read, or NULL: drafts for all.  A negative one: no response, nothing of it is
+ *                read, n_accepted 0, tokens -1 and log-probs 0.
+ *  temperature, draft_temperature  > 0.
+ *  tokens_out    [batch, drafts + 1] i64, device, written: y_0 .. y_{n-1}, t, then -1.
+ *  n_accepted_out [batch] i32, device, written: n.
+ *  logprobs_out  [batch, drafts + 1] f32, device, written: log p_i of the token in place i; 0 behind place n.
+ * Logits of -inf (or of the type's lowest value) have no probability.  Where w has no sum, or it is no number
+ * (a row of -inf throughout, with +inf or NaN, in either of the two), t is -1 and its log-prob NaN.
+ * Probabilities and sums are fp64, in a fixed order: t does not depend on rounding short of 1e-12 of its border.
+ * drafts in [0, 64]; vocab in [1, 2^28].  workspace: device, 256-byte aligned, at least
+ * grpo_verify_workspace_bytes(...) bytes (0 for invalid sizes), contents ignored.  batch == 0 does nothing.
+ * ------------------------------------------------------------------------- */
+size_t grpo_verify_workspace_bytes(int64_t batch, int64_t drafts, int64_t vocab, grpo_dtype dtype);
+grpo_status grpo_verify_drafts(const void *target_logits, int64_t target_batch_stride, int64_t target_row_stride,
+                               const void *draft_logits, int64_t draft_batch_stride, int64_t draft_row_stride,
+                               grpo_dtype dtype, int64_t batch, int64_t drafts, int64_t vocab,
+                               const int64_t *draft_tokens, const float *accept_u, const double *sample_u,
+                               const int32_t *draft_lengths, double temperature, double draft_temperature,
+                               int64_t *tokens_out, int32_t *n_accepted_out, float *logprobs_out,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------- *
  * The norms around a block of the model, with the block's gate and the scale it is added
  * to the residual stream with: the block's output f is normed, weighted, gated, scaled and
  * added, and the sum is normed for what follows (the next block, or the head: h is

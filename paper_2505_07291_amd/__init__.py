@@ -10,6 +10,6 @@ from .binding import (COUNT_NAMES, GRPO_BF16, GRPO_F32, GrpoError, grpo_filter_g
                       grpo_workspace_error, lib, status_string,
                       grpo_lmhead_workspace_bytes, grpo_lmhead_workspace_bytes_for_chunk, grpo_lmhead_logprobs_fwd, grpo_lmhead_loss_fwd_bwd,
                       grpo_lmhead_loss_aux_fwd_bwd,
-                      grpo_block_norm_fwd, grpo_block_norm_bwd, OptimPlan, grpo_optim_plan, grpo_grad_norm, grpo_adamw_step)
+                      grpo_verify_drafts, grpo_block_norm_fwd, grpo_block_norm_bwd, OptimPlan, grpo_optim_plan, grpo_grad_norm, grpo_adamw_step)
 from .build import build_library  # noqa: F401
 from . import workloads  # noqa: F401

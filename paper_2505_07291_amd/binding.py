@@ -125,6 +125,10 @@ def _load_lib():
     L.grpo_lmhead_loss_aux_fwd_bwd.argtypes = [vp, i64, vp, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp,
                                                f32, f32, f32, f32, f32, f32, f64, f32, vp, vp, vp, vp,
                                                vp, i64, vp, i64, i32, vp, sz, vp]
+    L.grpo_verify_workspace_bytes.restype = sz
+    L.grpo_verify_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    L.grpo_verify_drafts.restype = i32
+    L.grpo_verify_drafts.argtypes = [vp, i64, i64, vp, i64, i64, i32, i64, i64, i64, vp, vp, vp, vp, f64, f64, vp, vp, vp, vp, sz, vp]
     L.grpo_block_norm_fwd.restype = i32
     L.grpo_block_norm_fwd.argtypes = [vp, i64, i32, vp, i64, vp, vp, i64, vp, i32, i64, i64, f64, f64, vp, i64, vp, i64, vp]
     L.grpo_block_norm_workspace_bytes.restype = sz
@@ -678,6 +682,75 @@ def grpo_lmhead_loss_aux_fwd_bwd(hidden, weight, tokens, old_logprobs, ref_logpr
     if rc != GRPO_OK:
         raise GrpoError(rc, "grpo_lmhead_loss_aux_fwd_bwd")
     return loss_out, logprobs_out, entropy_out, counts_out, grad_hidden, grad_weight
+
+
+def _verify_logits(t, name, batch, rows, vocab, dtype, device):
+    """The strides of responses and of rows of [batch, rows, vocab] logits, in elements."""
+    if t.dim() != 3 or t.dtype != dtype or tuple(t.shape) != (batch, rows, vocab) or (t.stride(2) != 1 and vocab > 1):
+        raise ValueError("%s must be a %s tensor [%d, %d, %d] with unit stride along the vocabulary" % (name, dtype, batch, rows, vocab))
+    if t.device != device:
+        raise ValueError("%s must live on %s" % (name, device))
+    # a stride that nothing is behind can be anything
+    per16 = 8 if dtype == torch.bfloat16 else 4
+    return (t.stride(0) if batch > 1 else 0), (t.stride(1) if rows > 1 else (vocab + per16 - 1) // per16 * per16)
+
+
+def _check_2d(t, dtype, shape, name, device):
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor %s" % (name, dtype, list(shape)))
+    if t.device != device:
+        raise ValueError("%s must live on %s" % (name, device))
+
+
+def grpo_verify_drafts(target_logits, draft_logits, draft_tokens, accept_u, sample_u, draft_lengths=None, temperature=1.0,
+                       draft_temperature=1.0, *, tokens_out=None, n_accepted_out=None, logprobs_out=None, workspace=None, stream=None):
+    """Verifies drafted tokens and samples the one behind them; see grpo_verify_drafts in grpo.h.
+
+    target_logits [batch, drafts + 1, vocab] bf16 or f32; draft_logits [batch, drafts, vocab] of the same dtype, or None for
+    tokens that no model drafted; draft_tokens [batch, drafts] i64 and accept_u [batch, drafts] f32 (either may be None without
+    drafts); sample_u [batch] f64; draft_lengths [batch] i32 or None.  Returns (tokens [batch, drafts + 1] i64,
+    n_accepted [batch] i32, logprobs [batch, drafts + 1] f32)."""
+    if not target_logits.is_cuda:
+        raise ValueError("target_logits must be a device tensor: libgrpo has no CPU path")
+    if target_logits.dim() != 3 or target_logits.dtype not in _DTYPE_CODES or target_logits.shape[1] < 1:
+        raise ValueError("target_logits must be a bfloat16 or float32 tensor [batch, drafts + 1, vocab]")
+    dev, dtype = target_logits.device, target_logits.dtype
+    n, k, v = target_logits.shape[0], target_logits.shape[1] - 1, target_logits.shape[2]
+    tb, tk = _verify_logits(target_logits, "target_logits", n, k + 1, v, dtype, dev)
+    db = dk = 0
+    if k == 0:
+        draft_logits = None
+    if draft_logits is not None:
+        db, dk = _verify_logits(draft_logits, "draft_logits", n, k, v, dtype, dev)
+    for t, dt, name in ((draft_tokens, torch.int64, "draft_tokens"), (accept_u, torch.float32, "accept_u")):
+        if t is not None:
+            _check_2d(t, dt, (n, k), name, dev)
+        elif k > 0:
+            raise ValueError("%s is needed where there are drafts" % name)
+    _check(sample_u, torch.float64, n, "sample_u", dev)
+    if draft_lengths is not None:
+        _check(draft_lengths, torch.int32, n, "draft_lengths", dev)
+    if tokens_out is None:
+        tokens_out = torch.empty((n, k + 1), dtype=torch.int64, device=dev)
+    else:
+        _check_2d(tokens_out, torch.int64, (n, k + 1), "tokens_out", dev)
+    if n_accepted_out is None:
+        n_accepted_out = torch.empty(n, dtype=torch.int32, device=dev)
+    else:
+        _check(n_accepted_out, torch.int32, n, "n_accepted_out", dev)
+    if logprobs_out is None:
+        logprobs_out = torch.empty((n, k + 1), dtype=torch.float32, device=dev)
+    else:
+        _check_2d(logprobs_out, torch.float32, (n, k + 1), "logprobs_out", dev)
+    L, code = lib(), _DTYPE_CODES[dtype]
+    if workspace is None:
+        workspace = torch.empty(L.grpo_verify_workspace_bytes(n, k, v, code), dtype=torch.uint8, device=dev)
+    rc = L.grpo_verify_drafts(_ptr(target_logits), tb, tk, _ptr(draft_logits), db, dk, code, n, k, v, _ptr(draft_tokens), _ptr(accept_u),
+                              _ptr(sample_u), _ptr(draft_lengths), float(temperature), float(draft_temperature), _ptr(tokens_out),
+                              _ptr(n_accepted_out), _ptr(logprobs_out), _ptr(workspace), workspace.numel(), _raw_stream(stream, dev.index))
+    if rc != GRPO_OK:
+        raise GrpoError(rc, "grpo_verify_drafts")
+    return tokens_out, n_accepted_out, logprobs_out
 
 
 _DTYPE_CODES = {torch.float32: GRPO_F32, torch.bfloat16: GRPO_BF16}

@@ -3085,4 +3085,5 @@ grpo_status grpo_workspace_error(const void *workspace, int32_t *flag_out, void 
 #include "lmhead.hpp"
 #include "optim.hpp"
 #include "blocknorm.hpp"
+#include "verify.hpp"
 #endif  // GRPO_ROWS_OF

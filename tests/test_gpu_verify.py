@@ -1,0 +1,275 @@
+"""Verification of drafted tokens against its definition, one response after the other in fp64 on the CPU.
+
+Tokens and counts are compared as they are: both sides form probabilities and sums in fp64, which agree to about 1e-13, so that a
+random number would have to lie within that of a border.  Log-probs are rounded to fp32 once, 2^-24 of their value; 1e-9 covers
+what fp64 loses in front of that."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2505_07291_amd as grpo
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def softmax(row, temperature):
+    z = row.astype(np.float64) / temperature
+    with np.errstate(all="ignore"):
+        e = np.exp(z - z.max())
+        return e / e.sum()
+
+
+def reference(target, draft, tokens, u, v, lengths, t=1.0, td=1.0):
+    target = target.float().cpu().numpy()
+    draft = None if draft is None else draft.float().cpu().numpy()
+    tokens, u, v = tokens.cpu().numpy(), u.cpu().double().numpy(), v.cpu().numpy()
+    n, k1, vocab = target.shape
+    out, lps, acc = np.full((n, k1), -1, np.int64), np.zeros((n, k1)), np.zeros(n, np.int32)
+    for b in range(n):
+        k = k1 - 1 if lengths is None else min(int(lengths[b]), k1 - 1)
+        if k < 0:
+            continue
+        for i in range(k + 1):
+            p = softmax(target[b, i], t)
+            w = p
+            if i < k:
+                y = int(tokens[b, i])
+                known = 0 <= y < vocab
+                q = softmax(draft[b, i], td) if draft is not None else np.where(np.arange(vocab) == y, 1.0, 0.0)
+                qy = (q[y] if known else 0.0) if draft is not None else 1.0
+                if u[b, i] * qy < (p[y] if known else 0.0):
+                    out[b, i], lps[b, i] = y, np.log(p[y])
+                    continue
+                w = np.where(p - q > 0, p - q, np.where(np.isnan(p - q), np.nan, 0.0))
+                if w.sum() == 0:
+                    w = p
+            acc[b] = i
+            c = np.cumsum(w)
+            if not c[-1] > 0:
+                out[b, i], lps[b, i] = -1, np.nan
+            else:
+                j = int(np.searchsorted(c, v[b] * c[-1], side="right"))
+                out[b, i] = j if j < vocab else np.flatnonzero(w)[-1]
+                lps[b, i] = np.log(p[out[b, i]])
+            break
+    return out, acc, lps
+
+
+def check(target, draft, tokens, u, v, lengths=None, t=1.0, td=1.0):
+    dev = lambda x: None if x is None else x.cuda() if not x.is_cuda else x  # noqa: E731
+    got = grpo.grpo_verify_drafts(dev(target), dev(draft), dev(tokens), dev(u), dev(v), dev(lengths), temperature=t, draft_temperature=td)
+    out, acc, lps = reference(target, draft, tokens, u, v, lengths, t, td)
+    assert np.array_equal(got[1].cpu().numpy(), acc)
+    assert np.array_equal(got[0].cpu().numpy(), out)
+    lp = got[2].cpu().double().numpy()
+    assert np.array_equal(np.isnan(lp), np.isnan(lps))
+    off = np.abs(np.nan_to_num(lp) - np.nan_to_num(lps))
+    assert (off <= 2.0 ** -24 * np.abs(np.nan_to_num(lps)) + 1e-9).all(), off.max()
+    return got
+
+
+def rows(z, dtype, pad=0):
+    """Logits whose rows begin on 16-byte boundaries, `pad` 16 bytes further apart than they need be."""
+    n, k, v = z.shape
+    per16 = 8 if dtype == BF16 else 4
+    pitch = (v + per16 - 1) // per16 * per16 + pad * per16
+    t = torch.full((n, k, pitch), float("nan"), dtype=dtype)
+    t[:, :, :v] = z.to(dtype)
+    return t.cuda()[:, :, :v]
+
+
+def make(seed, n, k, v, dtype=BF16, draft=True, near=0.5, sharp=3.0, pad=0):
+    g = torch.Generator().manual_seed(seed)
+    z = torch.randn((n, k + 1, v), generator=g) * sharp
+    q = z[:, :k] + torch.randn((n, k, v), generator=g) * near
+    noise = -torch.log(-torch.log(torch.rand((n, k, v), generator=g).clamp(1e-20, 1 - 1e-7)))
+    tokens = (q + noise).argmax(-1) if k else torch.zeros((n, 0), dtype=torch.int64)
+    return (rows(z, dtype, pad), rows(q, dtype, pad) if draft else None, tokens, torch.rand((n, k), generator=g),
+            torch.rand((n,), generator=g, dtype=torch.float64))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("n,k,v", [(1, 0, 1), (3, 0, 7), (2, 1, 2), (5, 2, 9), (64, 3, 33), (7, 4, 1000), (9, 8, 2047), (9, 1, 2048),
+                                   (9, 2, 2049), (4, 5, 16391), (300, 0, 4100), (40, 6, 5000), (2, 64, 300), (1, 1, 152064), (2, 2, 300007)])
+def test_sizes(n, k, v, draft, dtype):
+    check(*make(n + 7 * k + v, n, k, v, dtype, draft), t=0.8, td=1.25)
+
+
+def test_many_rows_in_large_parts():
+    check(*make(1, 330, 3, 20011))
+
+
+@pytest.mark.parametrize("draft", [True, False])
+def test_lengths(draft):
+    a = make(5, 12, 4, 777, draft=draft, near=0.1)
+    check(*a, torch.tensor([0, 1, 2, 3, 4, 5, 100, -1, -7, 4, 4, 0], dtype=torch.int32))
+
+
+def test_rows_behind_the_drafts_are_not_read():
+    target, draft, tokens, u, v = make(6, 6, 3, 500, near=0.1)
+    lengths = torch.tensor([0, 1, 2, 3, -1, 2], dtype=torch.int32)
+    want = check(target, draft, tokens, u, v, lengths)
+    for b, k in enumerate(lengths.tolist()):
+        target[b, k + 1:] = float("nan")
+        draft[b, max(k, 0):] = float("nan")
+        tokens[b, max(k, 0):] = -12345
+    got = grpo.grpo_verify_drafts(target, draft, tokens.cuda(), u.cuda(), v.cuda(), lengths.cuda())
+    assert all(torch.equal(x, y) for x, y in zip(want, got))
+
+
+def test_pitches_and_order_of_strides():
+    target, draft, tokens, u, v = make(8, 5, 3, 1003, pad=2)
+    want = check(target, draft, tokens, u, v)
+    # positions outermost: [drafts + 1, batch, vocab] as an engine that steps through positions keeps them
+    turned = rows(target.transpose(0, 1).cpu().float(), BF16).transpose(0, 1)
+    got = grpo.grpo_verify_drafts(turned, draft, tokens.cuda(), u.cuda(), v.cuda())
+    assert all(torch.equal(x, y) for x, y in zip(want, got))
+    # the same logits for all responses
+    one = target[:1].expand(5, -1, -1)
+    check(one, draft, tokens, u, v)
+
+
+def test_offsets_beyond_32_bits():
+    v = 4096
+    z = torch.randn((2, 1, v), generator=torch.Generator().manual_seed(1))
+    far = 2500000000 // 8 * 8
+    big = torch.empty(far + v, dtype=BF16, device="cuda")
+    t = big.as_strided((2, 1, v), (far, v, 1))
+    t.copy_(z)
+    none = torch.zeros((2, 0), dtype=torch.int64)
+    check(t, None, none, none.float(), torch.tensor([0.3, 0.6], dtype=torch.float64))
+
+
+def test_borders_of_the_sums():
+    """Equal logits have exact sums: a random number on a border belongs to the token behind it; next to 1 to the last token."""
+    z = torch.full((8, 1, 8), 2.0)
+    z[:, :, [3, 7]] = float("-inf")  # without probability, at the end too
+    v = torch.tensor([0.0, 1 / 6, 0.25, 0.5, 0.75, 5 / 6, 1 - 2.0 ** -53, 0.999], dtype=torch.float64)
+    none = torch.zeros((8, 0), dtype=torch.int64)
+    # (not against the reference: it divides by the sum first, and sixths added up are not exact)
+    got = grpo.grpo_verify_drafts(rows(z, F32), None, none.cuda(), none.float().cuda(), v.cuda())
+    assert got[0][:, 0].tolist() == [0, 1, 1, 4, 5, 6, 6, 6]
+
+
+def test_ratios_at_their_borders():
+    """u q < p with equality, q = 0, p = 0 and u = 0."""
+    low = float("-inf")
+    z = torch.tensor([[0.0, 0.0, 0.0, 0.0], [0.0, 0.0, 0.0, 0.0], [0.0, low, 0.0, 0.0], [0.0, 0.0, low, low], [0.0, low, 0.0, low]])
+    q = torch.tensor([[0.0, 0.0, low, low], [0.0, 0.0, low, low], [0.0, low, 0.0, 0.0], [low, low, 0.0, 0.0], [0.0, 0.0, low, low]])
+    target = torch.zeros((5, 2, 4))
+    target[:, 0] = z
+    tokens = torch.tensor([[0], [0], [1], [0], [1]])
+    u = torch.tensor([[0.5], [0.49999997], [0.0], [0.9], [0.0]])
+    v = torch.full((5,), 0.5, dtype=torch.float64)
+    got = check(rows(target, F32), rows(q[:, None], F32), tokens, u, v)
+    # 0.5 * 0.5 is not below 0.25; p = q = 0 is not accepted; p > 0 = q always is; p = 0 never
+    assert got[1].tolist() == [0, 1, 0, 1, 0]
+
+
+def test_the_same_distributions():
+    """p = q: every draft is accepted, whatever its number; with p = q and a draft outside the vocabulary nothing is left of p - q."""
+    target, _, tokens, _, v = make(3, 50, 4, 301)
+    u = torch.full((50, 4), 1 - 2.0 ** -24)
+    got = check(target, target[:, :4], tokens, u, v)
+    assert (got[1] == 4).all()
+    tokens[:25, 2], tokens[25:, 2] = 301, -1
+    got = check(target, target[:, :4], tokens, u, v)
+    assert (got[1] == 2).all() and (got[0][:, 2] >= 0).all() and torch.isfinite(got[2]).all()
+
+
+def test_a_token_drafted_without_a_model_is_never_sampled_again():
+    target, _, tokens, _, v = make(4, 200, 2, 12, sharp=0.5)
+    u = torch.full((200, 2), 0.9999)
+    got = check(target, None, tokens, u, v)
+    assert (got[1] == 0).all() and not (got[0][:, 0].cpu() == tokens[:, 0]).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_masked_logits(dtype):
+    """Most of the vocabulary masked by -inf or by the type's lowest value, whole parts of a row among it."""
+    for low in (float("-inf"), torch.finfo(dtype).min):
+        target, draft, tokens, u, v = make(9, 6, 3, 9000, dtype)
+        keep = torch.zeros((1, 1, 9000), dtype=torch.bool)
+        keep[..., [5, 4000, 4001, 8999]] = True
+        keep = keep.cuda()
+        target.masked_fill_(~keep, low)
+        draft.masked_fill_(~keep, low)
+        tokens[:, :] = torch.tensor([5, 4001, 8999])
+        check(target, draft, tokens, u, v)
+
+
+def test_rows_with_nothing_in_them_infinities_and_nan():
+    target, draft, tokens, u, v = make(10, 9, 2, 5001, near=0.01)
+    target[1, 0] = float("-inf")
+    target[2, 1, 77] = float("nan")
+    target[3, 2, 4000] = float("inf")
+    target[4, 2] = float("-inf")
+    draft[5, 1] = float("-inf")
+    draft[6, 0, 3] = float("nan")
+    draft[7, 0, 3] = float("inf")
+    u[:] = 0.5
+    got = check(target, draft, tokens, u, v)
+    assert (got[0][torch.arange(9), got[1].long()] == -1).tolist()[:8] == [False, True, True, True, True, True, True, True]
+    assert torch.isfinite(got[2][0]).all() and torch.isfinite(got[2][8]).all()
+
+
+def test_tokens_are_distributed_as_the_target():
+    """A poor draft model: the accepted and the resampled first tokens together follow the target (chi-square, 31 degrees of
+    freedom: beyond 70 once in 10^4 seeds, and this one is fixed)."""
+    n, vocab = 40000, 32
+    g = torch.Generator().manual_seed(12)
+    z, q = torch.randn(vocab, generator=g) * 1.5, torch.randn(vocab, generator=g) * 1.5
+    tokens = torch.multinomial(torch.softmax(q, 0), n, replacement=True, generator=g)[:, None]
+    target = rows(z.expand(1, 2, vocab), F32).expand(n, 2, vocab)
+    draft = rows(q.expand(1, 1, vocab), F32).expand(n, 1, vocab)
+    got = grpo.grpo_verify_drafts(target, draft, tokens.cuda(), torch.rand((n, 1), generator=g).cuda(),
+                                  torch.rand(n, generator=g, dtype=torch.float64).cuda())
+    seen = torch.bincount(got[0][:, 0].cpu(), minlength=vocab).double()
+    want = torch.softmax(z.double(), 0) * n
+    assert 0.2 < got[1].double().mean() < 0.8
+    assert ((seen - want) ** 2 / want).sum() < 70
+
+
+def test_nothing_to_do():
+    e = lambda *s, dtype=F32: torch.zeros(s, dtype=dtype, device="cuda")  # noqa: E731
+    got = grpo.grpo_verify_drafts(e(0, 3, 10), e(0, 2, 10), e(0, 2, dtype=torch.int64), e(0, 2), e(0, dtype=torch.float64))
+    assert [tuple(t.shape) for t in got] == [(0, 3), (0,), (0, 3)]
+
+
+@pytest.mark.parametrize("n,k", [(4, 0), (1, 4), (48, 3)])
+def test_captured_and_replayed(n, k):
+    target, draft, tokens, u, v = (None if t is None else t.cuda() for t in make(13, n, k, 50257, draft=k > 0))
+    call = lambda: grpo.grpo_verify_drafts(target, draft, tokens, u, v)  # noqa: E731
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = call()
+    for i in range(4):
+        v.add_(0.23).frac_()
+        u.add_(0.31).frac_()
+        want = call()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, out)), i
+
+
+def test_on_two_streams_at_once():
+    a = [t.cuda() for t in make(14, 8, 3, 152064)]
+    b = [t.cuda() for t in make(15, 8, 3, 152064)]
+    want = [grpo.grpo_verify_drafts(*x) for x in (a, b)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = []
+        for x, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                got.append(grpo.grpo_verify_drafts(*x))
+        torch.cuda.synchronize()
+        for x, y in zip(want, got):
+            assert all(torch.equal(s, t) for s, t in zip(x, y))
