@@ -25,39 +25,58 @@ struct BlockNorm {
     float scale, eps, inv_d;
 };
 
-// VEC neighbours of a row, in fp32; zeros behind its end.
+// VEC neighbours of a row as they lie in memory: 16 bytes, or 8 of bf16 beside 16 of fp32.
 template <grpo_dtype DT, int VEC>
+struct RawVec {
+    static_assert(VEC == Elem<DT>::EPV, "16 bytes");
+    u32x4 v;
+    __device__ __forceinline__ void get(float (&f)[VEC]) const { unpack<DT>(v, f); }
+    __device__ __forceinline__ void set(const float (&f)[VEC]) { v = pack<DT>(f); }
+};
+template <>
+struct RawVec<GRPO_BF16, 4> {
+    u32x2 v;
+    __device__ __forceinline__ void get(float (&f)[4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            f[2 * i] = as_f32(v[i] << 16);
+            f[2 * i + 1] = as_f32(v[i] & 0xffff0000u);
+        }
+    }
+    __device__ __forceinline__ void set(const float (&f)[4]) { v = u32x2{bf16_pair(f[0], f[1]), bf16_pair(f[2], f[3])}; }
+};
+
+// The neighbours from column col on.  RAGGED: the row may end inside them; zeros behind its end.  ONCE: nobody reads them again.
+template <grpo_dtype DT, int VEC, bool RAGGED = true, bool ONCE = true>
+__device__ __forceinline__ RawVec<DT, VEC> raw_load(const char *row, int col, int d)
+{
+    RawVec<DT, VEC> r;
+    if (!RAGGED || col + VEC <= d) {
+        typedef decltype(r.v) V;
+        const V *at = (const V *)(row + (size_t)col * Elem<DT>::BYTES);
+        r.v = ONCE ? __builtin_nontemporal_load(at) : *at;
+    } else {
+        float f[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f[i] = col + i < d ? load_elem<DT>(row, col + i) : 0.f;
+        r.set(f);
+    }
+    return r;
+}
+template <grpo_dtype DT, int VEC, bool RAGGED = true>
 __device__ __forceinline__ void row_load(const char *row, int col, int d, float (&v)[VEC])
 {
-    constexpr int B = Elem<DT>::BYTES;
-    if (col + VEC <= d) {
-        if constexpr (VEC * B == 16) {
-            unpack<DT>(*(const u32x4 *)(row + (size_t)col * B), v);
-        } else {
-            static_assert(DT == GRPO_BF16 && VEC == 4, "four bf16 values beside four fp32 ones");
-            const u32x2 u = *(const u32x2 *)(row + (size_t)col * B);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                v[2 * i] = as_f32(u[i] << 16);
-                v[2 * i + 1] = as_f32(u[i] & 0xffff0000u);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = col + i < d ? load_elem<DT>(row, col + i) : 0.f;
-    }
+    raw_load<DT, VEC, RAGGED, false>(row, col, d).get(v);  // weights, and rows that are read again
 }
-template <grpo_dtype DT, int VEC>
+template <grpo_dtype DT, int VEC, bool RAGGED = true>
 __device__ __forceinline__ void row_store(char *row, int col, int d, const float (&v)[VEC])
 {
-    constexpr int B = Elem<DT>::BYTES;
-    if (col + VEC <= d) {
-        if constexpr (VEC * B == 16) {
-            *(u32x4 *)(row + (size_t)col * B) = pack<DT>(v);
-        } else {
-            const u32x2 u = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
-            *(u32x2 *)(row + (size_t)col * B) = u;
-        }
+    RawVec<DT, VEC> r;
+    if (!RAGGED || col + VEC <= d) {
+        typedef decltype(r.v) V;
+        r.set(v);
+        __builtin_nontemporal_store(r.v, (V *)(row + (size_t)col * Elem<DT>::BYTES));
     } else {
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
@@ -66,7 +85,121 @@ __device__ __forceinline__ void row_store(char *row, int col, int d, const float
 }
 
 constexpr int kNormBlock = 256;
+constexpr long long kNormFwdGrid = 65536;
 constexpr long long kNormGrid = 1024;  // workgroups of the backward at most, each with a row of partial sums
+
+// The sum over the TPR lanes that share a row, to all of them: a wavefront, or the workgroup (lds: a place for each wavefront that
+// nobody reads any more).
+template <int TPR>
+__device__ __forceinline__ float row_sum_of(float v, float *lds)
+{
+    if constexpr (TPR == 64)
+        return wave_sum(v);
+    else
+        return block_sum<TPR>(v, lds);
+}
+
+// Where a lane loads from: at column 0 if the row has none for it, and blank() takes out what would go into a sum.  Nothing is under
+// a condition but the stores: what is loaded under one is waited for where it ends, weights of every vector one after the other.
+template <bool RAGGED>
+__device__ __forceinline__ int held_column(int col, int d)
+{
+    return RAGGED || col < d ? col : 0;
+}
+template <grpo_dtype DT, int VEC>
+__device__ __forceinline__ void blank(RawVec<DT, VEC> &r, bool there)
+{
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(r.v) / 4); ++i) r.v[i] = there ? r.v[i] : 0u;
+}
+
+// The weights of a lane's columns, once for all of its rows.
+template <grpo_dtype DT, int VEC, int TPR, int NV, bool RAGGED>
+__device__ __forceinline__ void load_weights(const BlockNorm &p, int t, RawVec<DT, VEC> (&w1)[NV], RawVec<DT, VEC> (&w2)[NV])
+{
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
+        if (p.w1) w1[i] = raw_load<DT, VEC, RAGGED, false>(p.w1, col, p.d);
+        if (p.w2) w2[i] = raw_load<DT, VEC, RAGGED, false>(p.w2, col, p.d);
+    }
+}
+
+// Rows that stay in registers between the passes over them: TPR lanes to a row, NV vectors to a lane.
+template <grpo_dtype RT, grpo_dtype DT, int TPR, int NV, bool RAGGED>
+__global__ void __launch_bounds__(TPR < kNormBlock ? kNormBlock : TPR) block_norm_fwd_held(BlockNorm p)
+{
+    constexpr int VEC = Elem<RT>::EPV, BLOCK = TPR < kNormBlock ? kNormBlock : TPR, ROWS = BLOCK / TPR;
+    __shared__ float lds[2][2][BLOCK / 64];
+    const int t = threadIdx.x % TPR;
+    RawVec<DT, VEC> w1r[NV], w2r[NV];
+    load_weights<DT, VEC, TPR, NV, RAGGED>(p, t, w1r, w2r);
+    int turn = 0;
+    for (long long row = (long long)blockIdx.x * ROWS + threadIdx.x / TPR; row < p.n; row += (long long)gridDim.x * ROWS, turn ^= 1) {
+        const char *x = p.x + row * p.xs, *f = p.f ? p.f + row * p.fs : nullptr, *g = p.g ? p.g + row * p.gs : nullptr;
+        RawVec<RT, VEC> xr[NV];
+        RawVec<DT, VEC> fr[NV], gr[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
+            if (f) fr[i] = raw_load<DT, VEC, RAGGED>(f, col, p.d);
+            xr[i] = raw_load<RT, VEC, RAGGED>(x, col, p.d);
+            if (g) gr[i] = raw_load<DT, VEC, RAGGED>(g, col, p.d);
+        }
+        float r1 = p.scale;
+        if (p.w1) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                blank(fr[i], (i * TPR + t) * VEC < p.d);
+                float b[VEC];
+                fr[i].get(b);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sum += b[e] * b[e];
+            }
+            r1 *= 1.f / sqrtf(row_sum_of<TPR>(sum, lds[turn][0]) * p.inv_d + p.eps);
+        }
+        float sum = 0.f;
+        float v[NV][VEC];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const bool there = (i * TPR + t) * VEC < p.d;
+            const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
+            xr[i].get(v[i]);
+            if (f) {
+                float b[VEC], w[VEC];
+                fr[i].get(b);
+                if (p.w1) {
+                    w1r[i].get(w);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) b[e] *= w[e];
+                }
+                if (g) {
+                    gr[i].get(w);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) b[e] *= w[e];
+                }
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[i][e] += r1 * b[e];
+                if (there) row_store<RT, VEC, RAGGED>(p.xo + row * p.xos, col, p.d, v[i]);
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) sum += there ? v[i][e] * v[i][e] : 0.f;
+        }
+        if (!p.w2) continue;
+        const float r2 = 1.f / sqrtf(row_sum_of<TPR>(sum, lds[turn][1]) * p.inv_d + p.eps);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const bool there = (i * TPR + t) * VEC < p.d;
+            const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
+            float w[VEC];
+            w2r[i].get(w);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[i][e] *= r2 * w[e];
+            if (there) row_store<DT, VEC, RAGGED>(p.h + row * p.hs, col, p.d, v[i]);
+        }
+    }
+}
 
 // What is added to the residual stream, without the scale: the block's output, normed, weighted and gated.
 template <grpo_dtype DT, int VEC>
@@ -85,8 +218,9 @@ __device__ __forceinline__ void branch(const BlockNorm &p, const char *g, int co
     }
 }
 
+// Rows that are too wide to hold: read again for every pass.
 template <grpo_dtype RT, grpo_dtype DT>
-__global__ void __launch_bounds__(kNormBlock) block_norm_fwd_k(BlockNorm p)
+__global__ void __launch_bounds__(kNormBlock) block_norm_fwd_streamed(BlockNorm p)
 {
     constexpr int VEC = 16 / Elem<RT>::BYTES;
     __shared__ float lds[2][kNormBlock / 64];
@@ -132,8 +266,199 @@ __global__ void __launch_bounds__(kNormBlock) block_norm_fwd_k(BlockNorm p)
     }
 }
 
+// Three sums behind one barrier.
+template <int TPR>
+__device__ __forceinline__ void row_sum3_of(float &a, float &b, float &c, float (*lds)[4])
+{
+    a = wave_sum(a);
+    b = wave_sum(b);
+    c = wave_sum(c);
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) {
+            float *at = lds[threadIdx.x >> 6];
+            at[0] = a;
+            at[1] = b;
+            at[2] = c;
+        }
+        lds_barrier();
+        a = lds[0][0];
+        b = lds[0][1];
+        c = lds[0][2];
+#pragma unroll
+        for (int w = 1; w < TPR / 64; ++w) {
+            a += lds[w][0];
+            b += lds[w][1];
+            c += lds[w][2];
+        }
+    }
+}
+
+// Rows that stay in registers, and with them the sums over the workgroup's rows.
+template <grpo_dtype RT, grpo_dtype DT, int TPR, int NV, bool RAGGED>
+__global__ void __launch_bounds__(TPR < kNormBlock ? kNormBlock : TPR, 2) block_norm_bwd_held(BlockNorm p)
+{
+    constexpr int VEC = Elem<RT>::EPV, BLOCK = TPR < kNormBlock ? kNormBlock : TPR, ROWS = BLOCK / TPR;
+    __shared__ float lds[2][BLOCK / 64][4], lds_t[2][BLOCK / 64];
+    const int t = threadIdx.x % TPR;
+    float acc2[NV][VEC] = {}, acc1[NV][VEC] = {};
+    RawVec<RT, VEC> xr[NV], dr[NV];
+    RawVec<DT, VEC> hr[NV], fr[NV], gr[NV], w1r[NV], w2r[NV];
+    load_weights<DT, VEC, TPR, NV, RAGGED>(p, t, w1r, w2r);
+    const long long step = (long long)gridDim.x * ROWS;
+    long long row = (long long)blockIdx.x * ROWS + threadIdx.x / TPR;
+    for (int turn = 0; row < p.n; row += step, turn ^= 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
+            if (p.w2) {
+                xr[i] = raw_load<RT, VEC, RAGGED>(p.x + row * p.xs, col, p.d);
+                hr[i] = raw_load<DT, VEC, RAGGED>(p.dh + row * p.dhs, col, p.d);
+            }
+            if (p.f) fr[i] = raw_load<DT, VEC, RAGGED>(p.f + row * p.fs, col, p.d);
+            if (p.dxo) dr[i] = raw_load<RT, VEC, RAGGED>(p.dxo + row * p.dxos, col, p.d);
+            if (p.g) gr[i] = raw_load<DT, VEC, RAGGED>(p.g + row * p.gs, col, p.d);
+        }
+        float sx = 0.f, sax = 0.f, sf = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const bool there = (i * TPR + t) * VEC < p.d;
+            const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
+            float u[VEC], v[VEC], w[VEC];
+            if (p.w2) {
+                blank(xr[i], there);
+                xr[i].get(v);
+                hr[i].get(u);
+                w2r[i].get(w);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    sx += v[e] * v[e];
+                    sax += u[e] * w[e] * v[e];
+                }
+            }
+            if (p.w1) {
+                blank(fr[i], there);
+                fr[i].get(v);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) sf += v[e] * v[e];
+            }
+        }
+        row_sum3_of<TPR>(sx, sax, sf, lds[turn]);
+        const float r2 = p.w2 ? 1.f / sqrtf(sx * p.inv_d + p.eps) : 0.f;
+        const float c2 = sax * r2 * p.inv_d;  // mean(a y2)
+        const float r1 = p.w1 ? 1.f / sqrtf(sf * p.inv_d + p.eps) : 1.f;
+        float D[NV][VEC];
+        float sty = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const bool there = (i * TPR + t) * VEC < p.d;
+            const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
+            float u[VEC], v[VEC], w[VEC];
+            if (p.dxo) {
+                dr[i].get(D[i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) D[i][e] = 0.f;
+            }
+            if (p.w2) {
+                xr[i].get(v);
+                hr[i].get(u);
+                w2r[i].get(w);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float y2 = v[e] * r2;
+                    D[i][e] += r2 * (u[e] * w[e] - y2 * c2);
+                    acc2[i][e] += u[e] * y2;
+                }
+            }
+            if (there) row_store<RT, VEC, RAGGED>(p.dx + row * p.dxs, col, p.d, D[i]);
+            if (!p.f) continue;
+            // from here on D is s D, and with a weight and a gate t
+            fr[i].get(v);
+            float sy[VEC];  // s D y1
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                v[e] *= r1;
+                D[i][e] *= p.scale;
+                sy[e] = D[i][e] * v[e];
+            }
+            if (p.w1) {
+                w1r[i].get(w);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) w[e] = 1.f;
+            }
+            if (p.g) {
+                gr[i].get(u);
+                if (p.dg) {
+                    float dg[VEC];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) dg[e] = sy[e] * w[e];
+                    if (there) row_store<DT, VEC, RAGGED>(p.dg + row * p.dgs, col, p.d, dg);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) sy[e] *= u[e];
+                }
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) w[e] *= u[e];
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                acc1[i][e] += sy[e];
+                D[i][e] *= w[e];
+                sty += D[i][e] * v[e];
+            }
+        }
+        if (p.f) {
+            float c1 = 0.f;
+            if (p.w1) c1 = row_sum_of<TPR>(sty, lds_t[turn]) * p.inv_d * r1;  // mean(t y1) r1
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int col = (i * TPR + t) * VEC;
+                if (p.w1) {
+                    float v[VEC];
+                    fr[i].get(v);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) D[i][e] = r1 * (D[i][e] - v[e] * c1);
+                }
+                if (col < p.d) row_store<DT, VEC, RAGGED>(p.df + row * p.dfs, col, p.d, D[i]);
+            }
+        }
+    }
+    // one row of sums to a workgroup
+    float *part = p.part + (size_t)blockIdx.x * 2 * p.d;
+    if constexpr (ROWS == 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * TPR + t) * VEC;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (col + e < p.d) {
+                    part[col + e] = acc2[i][e];
+                    part[p.d + col + e] = acc1[i][e];
+                }
+        }
+    } else {
+        __shared__ float sums[TPR * NV * VEC];
+        for (int which = 0; which < 2; ++which) {
+            for (int r = 0; r < ROWS; ++r) {
+                if (threadIdx.x / TPR == r) {
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            float &s = sums[(i * TPR + t) * VEC + e];
+                            s = (r ? s : 0.f) + (which ? acc1[i][e] : acc2[i][e]);
+                        }
+                }
+                __syncthreads();
+            }
+            for (int col = threadIdx.x; col < p.d; col += BLOCK) part[(size_t)which * p.d + col] = sums[col];
+            __syncthreads();
+        }
+    }
+}
+
 template <grpo_dtype RT, grpo_dtype DT>
-__global__ void __launch_bounds__(kNormBlock) block_norm_bwd_k(BlockNorm p)
+__global__ void __launch_bounds__(kNormBlock) block_norm_bwd_streamed(BlockNorm p)
 {
     constexpr int VEC = 16 / Elem<RT>::BYTES;
     __shared__ float lds[4][kNormBlock / 64];
@@ -218,30 +543,39 @@ __global__ void __launch_bounds__(kNormBlock) block_norm_bwd_k(BlockNorm p)
     }
 }
 
-// The workgroups' sums, added up in fp64 in their order.  With one gate for all rows (or none) the second sum is that of
-// s D (.) y1, which gives both dw1, times the gate, and the gate's gradient, times w1.
+// The workgroups' sums, added up in fp64: 64 columns to a workgroup, a sixteenth of the sums to each of its wavefronts, which
+// then are added in their order.  With one gate for all rows (or none) the second sum is that of s D (.) y1, which gives both
+// dw1, times the gate, and the gate's gradient, times w1.
 template <grpo_dtype DT>
-__global__ void __launch_bounds__(256) block_norm_columns(const float *part, int blocks, int d, const char *w1, const char *gate_row,
-                                                          float *dw1, float *dgate_row, float *dw2, int accumulate)
+__global__ void __launch_bounds__(1024) block_norm_columns(const float *part, int blocks, int d, const char *w1, const char *gate_row,
+                                                           float *dw1, float *dgate_row, float *dw2, int accumulate)
 {
-    const int col = blockIdx.x * 256 + threadIdx.x;
-    if (col >= d) return;
-    if (dw2) {
-        double s = 0.0;
-        for (int b = 0; b < blocks; ++b) s += part[(size_t)b * 2 * d + col];
-        dw2[col] = accumulate ? dw2[col] + (float)s : (float)s;
+    __shared__ double lds[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int col = blockIdx.x * 64 + lane, which = blockIdx.y;
+    if (which == 0 ? !dw2 : !dw1 && !dgate_row) return;
+    double s = 0.0;
+    if (col < d) {
+        const float *at = part + (size_t)which * d + col;
+#pragma unroll 8
+        for (int b = wave; b < blocks; b += 16) s += (double)at[(size_t)b * 2 * d];
     }
-    if (dw1 || dgate_row) {
-        double s = 0.0;
-        for (int b = 0; b < blocks; ++b) s += part[(size_t)b * 2 * d + d + col];
-        if (dw1) {
-            const float v = (float)s * (gate_row ? load_elem<DT>(gate_row, col) : 1.f);
-            dw1[col] = accumulate ? dw1[col] + v : v;
-        }
-        if (dgate_row) {
-            const float v = (float)s * (w1 ? load_elem<DT>(w1, col) : 1.f);
-            dgate_row[col] = accumulate ? dgate_row[col] + v : v;
-        }
+    lds[wave][lane] = s;
+    __syncthreads();
+    if (wave != 0 || col >= d) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += lds[w][lane];
+    if (which == 0) {
+        dw2[col] = accumulate ? dw2[col] + (float)s : (float)s;
+        return;
+    }
+    if (dw1) {
+        const float v = (float)s * (gate_row ? load_elem<DT>(gate_row, col) : 1.f);
+        dw1[col] = accumulate ? dw1[col] + v : v;
+    }
+    if (dgate_row) {
+        const float v = (float)s * (w1 ? load_elem<DT>(w1, col) : 1.f);
+        dgate_row[col] = accumulate ? dgate_row[col] + v : v;
     }
 }
 
@@ -292,20 +626,60 @@ static BlockNorm block_norm_params(int rt, int dt, const void *x, int64_t xs, co
     return p;
 }
 
+// Which kernel takes rows of d: X(lanes to a row, vectors to a lane) of the list for 8 or 4 values to a vector, the first
+// that holds a row, else the streamed one.
+#define GRPO_NORM_FWD_8(X) X(64, 1) X(64, 2) X(256, 1) X(256, 2) X(320, 2) X(256, 4) X(512, 4)
+#define GRPO_NORM_FWD_4(X) X(64, 1) X(64, 2) X(64, 4) X(256, 2) X(256, 4) X(256, 5) X(256, 8) X(512, 8)
+#define GRPO_NORM_BWD_8(X) X(64, 1) X(64, 2) X(256, 1) X(256, 2) X(320, 2) X(512, 2)
+#define GRPO_NORM_BWD_4(X) X(64, 1) X(64, 2) X(64, 4) X(256, 2) X(256, 4) X(256, 5) X(512, 4) X(512, 5)
+#define GRPO_NORM_CASE(KERNEL, MOST, TPR, NV)                                                                                        \
+    if (p.d <= TPR * NV * Elem<RT>::EPV) {                                                                                           \
+        constexpr int BLOCK = TPR < kNormBlock ? kNormBlock : TPR, ROWS = BLOCK / TPR;                                              \
+        const long long blocks = (p.n + ROWS - 1) / ROWS, grid = blocks < MOST ? blocks : MOST;                                      \
+        if (p.d % Elem<RT>::EPV)                                                                                                     \
+            hipLaunchKernelGGL((KERNEL<RT, DT, TPR, NV, true>), dim3((unsigned)grid), dim3(BLOCK), 0, st, p);                        \
+        else                                                                                                                         \
+            hipLaunchKernelGGL((KERNEL<RT, DT, TPR, NV, false>), dim3((unsigned)grid), dim3(BLOCK), 0, st, p);                       \
+        return (int)grid;                                                                                                            \
+    }
 template <grpo_dtype RT, grpo_dtype DT>
-static void launch_block_norm_fwd(const BlockNorm &p, hipStream_t st)
+static int launch_block_norm_fwd(const BlockNorm &p, hipStream_t st)
 {
-    const long long grid = p.n < 65536 ? p.n : 65536;
-    hipLaunchKernelGGL((block_norm_fwd_k<RT, DT>), dim3((unsigned)grid), dim3(kNormBlock), 0, st, p);
+#define GRPO_NORM_FWD(TPR, NV) GRPO_NORM_CASE(block_norm_fwd_held, kNormFwdGrid, TPR, NV)
+    if constexpr (Elem<RT>::EPV == 8) {
+        GRPO_NORM_FWD_8(GRPO_NORM_FWD)
+    } else {
+        GRPO_NORM_FWD_4(GRPO_NORM_FWD)
+    }
+#undef GRPO_NORM_FWD
+    const long long grid = p.n < kNormFwdGrid ? p.n : kNormFwdGrid;
+    hipLaunchKernelGGL((block_norm_fwd_streamed<RT, DT>), dim3((unsigned)grid), dim3(kNormBlock), 0, st, p);
+    return (int)grid;
+}
+
+template <grpo_dtype RT, grpo_dtype DT>
+static int launch_block_norm_bwd_rows(const BlockNorm &p, hipStream_t st)  // workgroups, and rows of partial sums
+{
+    if (p.n == 0) return 0;
+#define GRPO_NORM_BWD(TPR, NV) GRPO_NORM_CASE(block_norm_bwd_held, kNormGrid, TPR, NV)
+    if constexpr (Elem<RT>::EPV == 8) {
+        GRPO_NORM_BWD_8(GRPO_NORM_BWD)
+    } else {
+        GRPO_NORM_BWD_4(GRPO_NORM_BWD)
+    }
+#undef GRPO_NORM_BWD
+    const long long grid = p.n < kNormGrid ? p.n : kNormGrid;
+    hipLaunchKernelGGL((block_norm_bwd_streamed<RT, DT>), dim3((unsigned)grid), dim3(kNormBlock), 0, st, p);
+    return (int)grid;
 }
 
 template <grpo_dtype RT, grpo_dtype DT>
 static void launch_block_norm_bwd(const BlockNorm &p, hipStream_t st, float *dw1, float *dgate_row, float *dw2, int accumulate)
 {
-    const long long grid = p.n < kNormGrid ? p.n : kNormGrid;
-    if (p.n > 0) hipLaunchKernelGGL((block_norm_bwd_k<RT, DT>), dim3((unsigned)grid), dim3(kNormBlock), 0, st, p);
-    hipLaunchKernelGGL((block_norm_columns<DT>), dim3((unsigned)((p.d + 255) / 256)), dim3(256), 0, st, p.part, (int)grid, p.d, p.w1,
-                       p.gs ? nullptr : p.g, dw1, dgate_row, dw2, accumulate);
+    const int blocks = launch_block_norm_bwd_rows<RT, DT>(p, st);
+    if (dw1 || dgate_row || dw2)
+        hipLaunchKernelGGL((block_norm_columns<DT>), dim3((unsigned)((p.d + 63) / 64), 2), dim3(1024), 0, st, p.part, blocks, p.d, p.w1,
+                           p.gs ? nullptr : p.g, dw1, dgate_row, dw2, accumulate);
 }
 
 }  // namespace grpo_impl
