@@ -486,13 +486,15 @@ grpo_status grpo_lmhead_loss_aux_fwd_bwd(const void *hidden, int64_t hidden_stri
  *  accept_u      [batch, drafts] f32, sample_u [batch] f64, device, read: uniform in [0, 1).
  *  draft_lengths [batch] i32, device, read, or NULL: drafts for all.  A negative one: no response, nothing of it is
  *                read, n_accepted 0, tokens -1 and log-probs 0.
- *  temperature, draft_temperature  > 0.
+ *  temperature, draft_temperature  in [1e-30, 1e30].
  *  tokens_out    [batch, drafts + 1] i64, device, written: y_0 .. y_{n-1}, t, then -1.
  *  n_accepted_out [batch] i32, device, written: n.
  *  logprobs_out  [batch, drafts + 1] f32, device, written: log p_i of the token in place i; 0 behind place n.
  * Logits of -inf (or of the type's lowest value) have no probability.  Where w has no sum, or it is no number
  * (a row of -inf throughout, with +inf or NaN, in either of the two), t is -1 and its log-prob NaN.
- * Probabilities and sums are fp64, in a fixed order: t does not depend on rounding short of 1e-12 of its border.
+ * Sums are formed in a fixed order.  What decides n and t is fp64 (fp32 where the two sides differ by more than 2^-15 of themselves): t does not
+ * depend on rounding short of 1e-12 of its border.  Log-probs of accepted tokens come from fp32 terms and are off by at most 2^-17, that
+ * of t is rounded from fp64.
  * drafts in [0, 64]; vocab in [1, 2^28].  workspace: device, 256-byte aligned, at least
  * grpo_verify_workspace_bytes(...) bytes (0 for invalid sizes), contents ignored.  batch == 0 does nothing.
  * ------------------------------------------------------------------------- */

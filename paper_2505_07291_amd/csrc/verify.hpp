@@ -5,26 +5,45 @@
 //   draft y_i is accepted iff u_i q_i(y_i) < p_i(y_i), up to the first one, n, that is not
 //   then one token: the smallest j with  sum_{l <= j} w_l > v sum_l w_l,  w = max(p_n - q_n, 0), or p_n behind the last draft
 //
-// Which token that is must not hang on the order in which 152064 terms are added up: with sums that are off by 1e-7 the
-// border of some token lies between two orders' results in one row of a hundred.  So probabilities and sums are formed in fp64,
-// in which that is one row in 10^8.
+// verify_rows_k forms, for the drafted positions, maxima and sums of exponentials in fp32 and is bound by reading the logits (96
+// responses with 5 drafts of 152064 bf16, 256 MB: 50 us, 5.1 TB/s).  That is enough for a ratio that is not within 2^-15 of its random
+// number (the others are decided in fp64), but not for the token: with sums that are off by 1e-7 the border of some of 152064 tokens lies
+// between two orders' results in one row of a hundred.
 //
-// A row is cut into `chunks` parts, each a workgroup's, so that a few rows fill the GPU too.  verify_rows_k forms each part's
-// maximum and its sum of exponentials; verify_pick_k's workgroups, one to a part again, each find n from them, add up the
-// part's w, and the last one of a response to do so finds the part in which the sum crosses v S, and in it the token.
-// Behind the last draft w = p_n, whose sums are there already: one workgroup finds the token.
+// verify_sums_k forms in fp64 what the token needs, of row n alone: then that is one in 10^8.  It is bound by fp64 arithmetic, 18
+// instructions an exponential, of which the GPU does 1.7e12 a second (29e12 lanes of fma, 35e12 of the others): that batch 40 us.
+// It reads its rows once.  p - q needs the rows' sums S_p and S_q, of which only those in fp32 are known before; so over the entries with
+// p > q by those, e_p and e_q are added up separately, to A and B, and A / S_p - B / S_q is formed when S_p and S_q are there.  What
+// may be on the wrong side by that is summed up too (N), and where it could matter, or little is left of A / S_p - B / S_q, the
+// sums are formed again with the ratio of S_p and S_q as it is.
+//
+// verify_pick_k, a workgroup to a response, finds the piece in which the sum crosses, and in it the token (5 to 9 us).  That the rows
+// behind a refused draft are read for nothing costs less than to follow it: counted by the workgroups' last one, with what it
+// takes to hand sums from one to another inside a launch, that batch took 128 us a call, and takes 96.
 
 namespace __attribute__((visibility("hidden"))) grpo_impl {
 
 constexpr int kVerifyBlock = 256;
 constexpr int kMaxDrafts = 64;
 constexpr int kMaxChunks = 1024;
-constexpr int kVerifySlots = 8;  // vectors of a row that a lane holds at a time
+constexpr int kVerifySlots = 8;   // vectors of a row that a lane of verify_rows_k holds at a time
+constexpr int kSumSlots = 2;      // and one of verify_sums_k, of each of two rows
+// Workgroups from which on they are given more entries each, up to eight times as many: 8 responses with 4 drafts (2400 workgroups of
+// verify_rows_k, 300 of verify_sums_k) 33 us a call and 41 from twice as many on, 96 with 5 drafts 96 and 97, and 101 from half as many on.
+constexpr int64_t kRowsEnough = 4096, kSumsEnough = 2048;
+// Ratios that fp32 sums do not decide.  A term 2^x of a sum is off by 2^-23 (the instruction) and by the roundings of z - m, of
+// 1 / T and of x, 0.7 |x| 2^-24 each, and those below 2^-40 of the largest make up less than 2^-22 of any sum of 2^18 or fewer; three
+// roundings in a vector's sum and one of the part's: 94 * 2^-24, under 2^-17, for each of the two rows.
+constexpr double kNearRatio = 0x1p-15;
+// And entries for which they do not say whether p > q: they are hardly ever off by more.
+constexpr double kNearSide = 0x1p-20;
+constexpr int kSums = 5;
 
-struct VerifyPart {  // of a part of a row: its maximum, and the sum of exp((z - max) / T)
-    double sum;
-    float max;
-    int pad;
+// Where a response's drafts end: row n, of a draft that is refused or (refused = 0) behind the last; and the rows' maxima.
+struct Refusal {
+    int n, refused;
+    float max_p, max_q;
+    double rho;  // S_p / S_q by the sums in fp32
 };
 
 struct Verify {
@@ -36,13 +55,13 @@ struct Verify {
     const int *lengths;
     int batch, drafts;
     long long vocab;
-    int pickers;               // verify_pick_k's workgroups to a response: the parts, or 1 where nothing is drafted
-    int chunks, chunk;         // parts of a row, and entries in one (of whole vectors of a whole workgroup)
-    double k, kd;              // log2(e) / T, of the target and of the draft
-    double inv_t;
-    VerifyPart *part;          // [batch][2 drafts + 1][chunks]: target rows, then draft rows
-    double *w;                 // [batch][chunks]: sums of the parts' w
-    unsigned *ticket;          // [batch]
+    int chunks, chunk;              // verify_rows_k: parts of a row, and entries in one (of whole vectors of a whole workgroup)
+    int pieces, piece, sum_blocks;  // verify_sums_k: pieces of row n, each a wavefront's, and entries in one; workgroups to a response
+    double k, kd;                   // log2(e) / T, of the target and of the draft
+    unsigned long long *part;       // [batch][2 drafts][chunks]: target rows, then draft rows; maximum, and sum of exp((z - maximum) / T)
+    double *sums;                   // [batch][pieces][kSums]: S_p, S_q, A, B, N of a piece of row n
+    float *tops;                    // [batch][pieces]: the maximum that S_p and A are relative to
+    Refusal *refusal;               // [batch]
     long long *tokens_out;
     int *accepted_out;
     float *logprobs_out;
@@ -54,7 +73,10 @@ struct Verify {
     }
     __device__ __forceinline__ const char *target_row(int b, int i) const { return target + b * tb + i * tk; }
     __device__ __forceinline__ const char *draft_row(int b, int i) const { return draft + b * db + i * dk; }
-    __device__ __forceinline__ const VerifyPart *parts(int b, int row) const { return part + ((long long)b * (2 * drafts + 1) + row) * chunks; }
+    __device__ __forceinline__ unsigned long long *parts(int b, int row) const
+    {
+        return part + ((long long)b * 2 * drafts + row) * chunks;
+    }
 };
 
 // EPV entries of a row from entry j on, -inf behind its end.
@@ -70,20 +92,131 @@ __device__ __forceinline__ void logits_load(const char *row, long long j, long l
     }
 }
 
-// exp((z - m) / T) with k = log2(e) / T.  A sum is kept relative to a maximum m; where nothing has been added yet, or all of it is
-// -inf, the maximum is -inf and 0 stands in for it in m's place: every z that is not NaN is -inf then and adds 0.
-__device__ __forceinline__ double exp_from(float z, float m, double k)
+// The same as they lie in memory.
+template <grpo_dtype DT>
+__device__ __forceinline__ u32x4 logits_raw(const char *row, long long j, long long to)
 {
-    return exp2(((double)z - (double)m) * k);
+    constexpr int EPV = Elem<DT>::EPV;
+    if (j + EPV <= to) return *(const u32x4 *)(row + j * Elem<DT>::BYTES);
+    float z[EPV];
+#pragma unroll
+    for (int i = 0; i < EPV; ++i) z[i] = j + i < to ? load_elem<DT>(row, j + i) : -INFINITY;
+    return pack<DT>(z);
 }
-__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
-// A wavefront's lanes' (max, sum) pairs become the whole's in every lane.
-__device__ __forceinline__ void wave_join(float &m, double &s, double k)
+// SLOTS vectors of a row for each of `lanes` lanes, neighbours at a time, from entry j0 on.  Where all of them are inside the row the loads
+// are under no condition: one that is under one is waited for where it ends, each of the vectors alone.
+template <grpo_dtype DT, int SLOTS>
+__device__ __forceinline__ void logits_raw(const char *row, long long j0, int lane, int lanes, long long to, u32x4 (&v)[SLOTS])
 {
-    const float top = wave_max(m);
-    s = wave_sum_dpp(s * exp_from(m, finite_max(top), k));
-    m = top;
+    constexpr int EPV = Elem<DT>::EPV;
+    if (j0 + (long long)SLOTS * lanes * EPV <= to) {
+        const char *at = row + (j0 + lane * EPV) * Elem<DT>::BYTES;
+#pragma unroll
+        for (int t = 0; t < SLOTS; ++t) v[t] = *(const u32x4 *)(at + t * lanes * 16);
+    } else {
+#pragma unroll
+        for (int t = 0; t < SLOTS; ++t) v[t] = logits_raw<DT>(row, j0 + (t * lanes + lane) * EPV, to);
+    }
+}
+
+// 2^x for x <= 0 or little more, to 4e-16 of the value: x = n + f with n whole and |f| <= 1/2, and for 2^f the polynomial of degree
+// 10 that agrees with it at the eleven Chebyshev points of [-1/2, 1/2] (one of them 0: 2^0 is 1).  Below 2^-1075 the result is 0,
+// for -inf too.  NaN is not carried: a sum's maximum is NaN if one of its terms is (see maximum).  18 fp64 instructions; the
+// library function takes some three times as many.
+__device__ __forceinline__ double exp2_f64(double x)
+{
+    constexpr double magic = 0x1.8p52;  // adding it leaves the whole part in the low bits
+    x = fmax(x, -1100.0);
+    const double r = x + magic;
+    const double f = x - (r - magic);
+    double q = 0x1.e606343d16a96p-28;
+    q = fma(q, f, 0x1.b675bc52c98b0p-24);
+    q = fma(q, f, 0x1.62bfd47ecba29p-20);
+    q = fma(q, f, 0x1.ffcb540682f51p-17);
+    q = fma(q, f, 0x1.430913096c64ap-13);
+    q = fma(q, f, 0x1.5d87fe9d7a3b5p-10);
+    q = fma(q, f, 0x1.3b2ab6fba1defp-7);
+    q = fma(q, f, 0x1.c6b08d703ce4ap-5);
+    q = fma(q, f, 0x1.ebfbdff82c598p-3);
+    q = fma(q, f, 0x1.62e42fefa3a19p-1);
+    q = fma(q, f, 1.0);
+    return ldexp(q, (int)(unsigned)__builtin_bit_cast(unsigned long long, r));
+}
+
+// The larger one, NaN if either is.
+__device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float wave_maximum(float v)
+{
+    v = maximum(v, dpp_move<0xB1, 0xf>(v, v));
+    v = maximum(v, dpp_move<0x4E, 0xf>(v, v));
+    v = maximum(v, dpp_move<0x141, 0xf>(v, v));
+    v = maximum(v, dpp_move<0x140, 0xf>(v, v));
+    v = maximum(v, dpp_move<0x142, 0xa>(-INFINITY, v));
+    v = maximum(v, dpp_move<0x143, 0xc>(-INFINITY, v));
+    return as_f32((unsigned)__builtin_amdgcn_readlane((int)as_u32(v), 63));
+}
+
+// exp((z - m) / T) with k = log2(e) / T, as 2^(z k - m k).  A sum is kept relative to a maximum m; where nothing has been added
+// yet, or all of it is -inf, the maximum is -inf and 0 stands in for it: every z is -inf then and adds 0.
+__device__ __forceinline__ double times_k(float m, double k) { return m == -INFINITY ? 0.0 : (double)m * k; }
+__device__ __forceinline__ double exp_from(float z, double mk, double k) { return exp2_f64(fma((double)z, k, -mk)); }
+
+// A maximum and a sum relative to it; whatever the sum, NaN if the maximum is +inf or NaN.
+struct RowSum {
+    float max;
+    double sum;
+};
+
+// A row's maximum and sum from its parts', by one wavefront.
+__device__ __forceinline__ RowSum row_sum(const unsigned long long *part, int chunks, double k)
+{
+    const int lane = threadIdx.x & 63;
+    float m = -INFINITY;
+    double s = 0.0;
+    for (int c = lane; c < chunks; c += 64) {
+        const unsigned long long q = part[c];
+        const float part_max = as_f32((unsigned)q), part_sum = as_f32((unsigned)(q >> 32));
+        const float top = maximum(m, part_max);
+        const double ref = times_k(top, k);
+        s = s * exp_from(m, ref, k) + (double)part_sum * exp_from(part_max, ref, k);
+        m = top;
+    }
+    const float top = wave_maximum(m);
+    s = wave_sum_dpp(s * exp_from(m, times_k(top, k), k));
+    return {top, top < INFINITY ? s : __builtin_nan("")};
+}
+
+// What a position's fp32 sums say about its draft, by one wavefront: the rows' sums, p(y) and q(y).
+struct Position {
+    RowSum p, q;
+    double py, qy;
+};
+template <grpo_dtype DT>
+__device__ __forceinline__ Position position(const Verify &p, int b, int i)
+{
+    Position r;
+    const long long y = p.tokens[(long long)b * p.drafts + i];
+    const bool in = y >= 0 && y < p.vocab;
+    const float zp = in ? load_elem<DT>(p.target_row(b, i), y) : 0.f;
+    const float zq = in && p.draft ? load_elem<DT>(p.draft_row(b, i), y) : 0.f;
+    r.p = row_sum(p.parts(b, i), p.chunks, p.k);
+    r.q = {0.f, 1.0};
+    r.py = in ? exp_from(zp, times_k(r.p.max, p.k), p.k) / r.p.sum : 0.0;
+    r.qy = 1.0;
+    if (p.draft) {
+        r.q = row_sum(p.parts(b, p.drafts + i), p.chunks, p.kd);
+        r.qy = in ? exp_from(zq, times_k(r.q.max, p.kd), p.kd) / r.q.sum : 0.0;
+    }
+    return r;
+}
+// u q < p, u q >= p, or too near to tell from fp32 sums.  NaN is refused.
+enum { kAccepted, kRefused, kNear };
+__device__ __forceinline__ int verdict(float u, const Position &r)
+{
+    const double a = (double)u * r.qy;
+    if (a < r.py * (1.0 - kNearRatio)) return kAccepted;
+    return a <= r.py * (1.0 + kNearRatio) && r.py > 0.0 ? kNear : kRefused;
 }
 
 template <grpo_dtype DT>
@@ -96,32 +229,40 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_rows_k(Verify p)
     const int rest = blockIdx.x / p.chunks;
     const int b = rest % p.batch, pos = rest / p.batch;  // positions in order, target and draft rows in turn
     const int i = p.draft ? pos >> 1 : pos;
-    const bool drafted = p.draft && (pos & 1);
-    const int len = p.length(b);
-    if (pos == 0 && c == 0 && threadIdx.x == 0) p.ticket[b] = 0;
-    if (drafted ? i >= len : i > len) return;
-    const char *row = drafted ? p.draft_row(b, i) : p.target_row(b, i);
-    const double k = drafted ? p.kd : p.k;
+    const bool of_draft = p.draft && (pos & 1);
+    if (i >= p.length(b)) return;
+    const char *row = of_draft ? p.draft_row(b, i) : p.target_row(b, i);
+    const double k = of_draft ? p.kd : p.k;
+    const float kf = (float)k;
     const long long from = (long long)c * p.chunk, to = from + p.chunk < p.vocab ? from + p.chunk : p.vocab;
     float m = -INFINITY;
-    double s = 0.0;
+    double s = 0.0;  // of sums of a vector's terms: long parts lose no more than short ones
     for (long long j0 = from; j0 < to; j0 += kVerifyBlock * EPV * kVerifySlots) {
-        float z[kVerifySlots][EPV];
+        u32x4 v[kVerifySlots];
         float top = m;
+        logits_raw<DT, kVerifySlots>(row, j0, threadIdx.x, kVerifyBlock, to, v);
 #pragma unroll
-        for (int t = 0; t < kVerifySlots; ++t) logits_load<DT>(row, j0 + (t * kVerifyBlock + threadIdx.x) * EPV, to, z[t]);
+        for (int t = 0; t < kVerifySlots; ++t) {
+            float z[EPV];
+            unpack<DT>(v[t], z);
 #pragma unroll
-        for (int t = 0; t < kVerifySlots; ++t)
-#pragma unroll
-            for (int e = 0; e < EPV; ++e) top = fmaxf(top, z[t][e]);
-        top = wave_max(top);
-        const float ref = finite_max(top);
-        s *= exp_from(m, ref, k);
+            for (int e = 0; e < EPV; ++e) top = maximum(top, z[e]);
+        }
+        top = wave_maximum(top);
+        const float ref = top == -INFINITY ? 0.f : top;
+        s *= exp_from(m, times_k(top, k), k);
 #pragma unroll
         for (int t = 0; t < kVerifySlots; ++t) {
             if (j0 + (long long)t * kVerifyBlock * EPV >= to) break;
+            float x[EPV];
+            unpack<DT>(v[t], x);
 #pragma unroll
-            for (int e = 0; e < EPV; ++e) s += exp_from(z[t][e], ref, k);
+            for (int e = 0; e < EPV; ++e) x[e] = __builtin_amdgcn_exp2f((x[e] - ref) * kf);
+#pragma unroll
+            for (int o = EPV / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int e = 0; e < o; ++e) x[e] += x[e + o];
+            s += (double)x[0];
         }
         m = top;
     }
@@ -134,304 +275,450 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_rows_k(Verify p)
     if (threadIdx.x == 0) {
         float top = lds_m[0];
 #pragma unroll
-        for (int w = 1; w < kVerifyBlock / 64; ++w) top = fmaxf(top, lds_m[w]);
+        for (int w = 1; w < kVerifyBlock / 64; ++w) top = maximum(top, lds_m[w]);
+        const double ref = times_k(top, k);
         s = 0.0;
 #pragma unroll
-        for (int w = 0; w < kVerifyBlock / 64; ++w) s += lds_s[w] * exp_from(lds_m[w], finite_max(top), k);
-        VerifyPart *out = p.part + ((long long)b * (2 * p.drafts + 1) + (drafted ? p.drafts + 1 + i : i)) * p.chunks + c;
-        out->max = top;
-        out->sum = s;
+        for (int w = 0; w < kVerifyBlock / 64; ++w) s += lds_s[w] * exp_from(lds_m[w], ref, k);
+        p.parts(b, of_draft ? p.drafts + i : i)[c] = (unsigned long long)as_u32((float)s) << 32 | as_u32(top);
     }
 }
 
-struct RowSum {
-    double sum;
-    float max;
-};
-
-// A row's maximum and sum from its parts', by one wavefront.
-__device__ __forceinline__ RowSum row_sum(const VerifyPart *part, int chunks, double k)
+// Sums of the lanes up to and with this one: within rows of 16, then over lane 15 of each row and lane 31.
+__device__ __forceinline__ double wave_scan(double v)
 {
-    const int lane = threadIdx.x & 63;
-    float m = -INFINITY;
-    double s = 0.0;
-    for (int c = lane; c < chunks; c += 64) {
-        const VerifyPart q = part[c];
-        const float top = fmaxf(m, q.max);
-        s = s * exp_from(m, finite_max(top), k) + q.sum * exp_from(q.max, finite_max(top), k);
-        m = top;
-    }
-    wave_join(m, s, k);
-    return {s, m};
-}
-
-struct Residual {  // what w is made of
-    const char *t, *d;  // target row, draft row (NULL: the draft has all of its mass on token y, or there is none: y = -1)
-    long long y;
-    double k, kd, inv_sp, inv_sq;
-    float mp, mq;
-};
-
-// w of EPV entries from entry j on.
-template <grpo_dtype DT>
-__device__ __forceinline__ void weights(const Residual &r, long long j, long long vocab, double (&w)[Elem<DT>::EPV])
-{
-#pragma clang fp contract(off)  // equal rows leave 0, not the rounding of one of the two products
-    constexpr int EPV = Elem<DT>::EPV;
-    float z[EPV];
-    logits_load<DT>(r.t, j, vocab, z);
-#pragma unroll
-    for (int e = 0; e < EPV; ++e) w[e] = exp_from(z[e], r.mp, r.k) * r.inv_sp;
-    if (r.d) {
-        logits_load<DT>(r.d, j, vocab, z);
-#pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-            w[e] -= exp_from(z[e], r.mq, r.kd) * r.inv_sq;
-            if (w[e] < 0.0) w[e] = 0.0;  // NaN stays
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < EPV; ++e)
-            if (j + e == r.y) w[e] = w[e] == w[e] ? 0.0 : w[e];
-    }
-}
-
-__device__ __forceinline__ double wave_scan(double v)  // sums of the lanes up to and with this one
-{
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const double up = __shfl_up(v, o, 64);
-        if (lane >= o) v += up;
-    }
+    v += dpp_move<0x111, 0xf>(v);
+    v += dpp_move<0x112, 0xf>(v);
+    v += dpp_move<0x114, 0xf>(v);
+    v += dpp_move<0x118, 0xf>(v);
+    v += dpp_move<0x142, 0xa>(v);
+    v += dpp_move<0x143, 0xc>(v);
     return v;
 }
+__device__ __forceinline__ double last_lane(double v)
+{
+    const long long b = __builtin_bit_cast(long long, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)b, 63), hi = (unsigned)__builtin_amdgcn_readlane((int)(b >> 32), 63);
+    return __builtin_bit_cast(double, (long long)(((unsigned long long)hi << 32) | lo));
+}
 
-struct PickLds {
-    double prefix[kMaxChunks];
-    double wave[kVerifyBlock / 64];
-    int part, found, last;
-    long long token;
+// Row n and what is taken off it: e_p = exp((z - max_p) / T) and e_q likewise, w = max(e_p - rho e_q, 0) with rho = S_p / S_q.
+struct Weights {
+    const char *t, *d;  // d: NULL where there is no draft row
+    long long y;        // without a draft row, the token that has all of the draft's mass; -1: none has
+    double k, kd, pk, qk, rho;
 };
 
-// The token: the parts' sums are in lds.prefix.  -1 where they have no sum, or it is no number.  All lanes take part and get it.
 template <grpo_dtype DT>
-__device__ long long pick_token(const Verify &p, const Residual &r, double v, PickLds &lds)
+__device__ __forceinline__ void weights(const Weights &r, long long j, long long to, double (&w)[Elem<DT>::EPV])
 {
     constexpr int EPV = Elem<DT>::EPV;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (tid == 0) {
-        lds.part = 0x7fffffff;
-        lds.last = -1;
-    }
-    __syncthreads();
-    double total = 0.0;
-    if (wave == 0) {
-        int last = -1;
-        for (int c0 = 0; c0 < p.chunks; c0 += 64) {
-            const int c = c0 + lane;
-            const double w = c < p.chunks ? lds.prefix[c] : 0.0;
-            if (w > 0.0) last = c;
-            const double up = total + wave_scan(w);
-            if (c < p.chunks) lds.prefix[c] = up;
-            total = __shfl(up, 63, 64);
-        }
-        atomicMax(&lds.last, last);
-    }
-    __syncthreads();
-    total = lds.prefix[p.chunks - 1];
-    if (!(total > 0.0) || !(total < INFINITY)) return -1;
-    const double target = v * total;
-    for (int c = tid; c < p.chunks; c += kVerifyBlock)
-        if (lds.prefix[c] > target) {
-            atomicMin(&lds.part, c);
-            break;
-        }
-    __syncthreads();
-    // a number next to 1 times the sum may be the sum: then the last token that has any
-    const int c = lds.part < p.chunks ? lds.part : lds.last;
-    __syncthreads();
-    if (tid == 0) lds.last = -1;
-    double base = c > 0 ? lds.prefix[c - 1] : 0.0;
-    const long long from = (long long)c * p.chunk, to = from + p.chunk < p.vocab ? from + p.chunk : p.vocab;
-    int fallback = -1;  // of this lane: its last entry with a weight
-    for (long long j0 = from; j0 < to; j0 += kVerifyBlock * EPV) {
-        const long long j = j0 + tid * EPV;
-        double w[EPV], sum = 0.0;
-        weights<DT>(r, j, to, w);
+    float z[EPV];
+    logits_load<DT>(r.t, j, to, z);
 #pragma unroll
-        for (int e = 0; e < EPV; ++e) {
-            sum += w[e];
-            if (w[e] > 0.0) fallback = (int)(j - from) + e;
-        }
-        const double up = wave_scan(sum);
-        if (lane == 63) lds.wave[wave] = up;
-        if (tid == 0) lds.found = 0x7fffffff;
-        __syncthreads();
-        double before = base;
+    for (int e = 0; e < EPV; ++e) w[e] = j + e == r.y ? 0.0 : exp_from(z[e], r.pk, r.k);
+    if (!r.d) return;
+    logits_load<DT>(r.d, j, to, z);
 #pragma unroll
-        for (int i = 0; i < kVerifyBlock / 64; ++i) {
-            if (i < wave) before += lds.wave[i];
-            base += lds.wave[i];
-        }
-        if (before + up > target) atomicMin(&lds.found, tid);
-        __syncthreads();
-        if (lds.found == tid) {  // the first lane whose entries cross; one of them does, up to rounding
-            double run = before + (up - sum);
-            int at = fallback;
+    for (int e = 0; e < EPV; ++e) w[e] = fmax(fma(-r.rho, exp_from(z[e], r.qk, r.kd), w[e]), 0.0);
+}
+
+// S_p, S_q, A, B and N of the entries from .. to, by one wavefront, which all of its lanes get.  With max_known r.pk and r.qk are those of the
+// rows' maxima; without, S_p is relative to the entries' own maximum, which becomes top, and there is nothing to take off.
+// EXACT: r.rho is S_p / S_q, and A becomes the sum of w.
+template <grpo_dtype DT, bool EXACT = false>
+__device__ __forceinline__ void part_sums(const Weights &r, long long from, long long to, bool max_known, float &top, double (&s)[kSums])
+{
+    constexpr int EPV = Elem<DT>::EPV;
+    const int lane = threadIdx.x & 63;
+    float m = -INFINITY;
+    double pk = r.pk;
 #pragma unroll
-            for (int e = EPV - 1; e >= 0; --e) {
-                double s = run;
+    for (int i = 0; i < kSums; ++i) s[i] = 0.0;
+    for (long long j0 = from; j0 < to; j0 += 64 * EPV * kSumSlots) {
+        u32x4 zr[kSumSlots], dr[kSumSlots];
+        logits_raw<DT, kSumSlots>(r.t, j0, lane, 64, to, zr);
+        if (r.d) logits_raw<DT, kSumSlots>(r.d, j0, lane, 64, to, dr);
+        if (!max_known) {
+            float now = m;
 #pragma unroll
-                for (int i = 0; i <= e; ++i) s += w[i];
-                if (s > target && w[e] > 0.0) at = (int)(j - from) + e;
+            for (int t = 0; t < kSumSlots; ++t) {
+                float z[EPV];
+                unpack<DT>(zr[t], z);
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) now = maximum(now, z[e]);
             }
-            lds.token = from + at;
+            now = wave_maximum(now);
+            pk = times_k(now, r.k);
+            s[0] *= exp_from(m, pk, r.k);
+            m = now;
         }
-        __syncthreads();
-        if (lds.found < kVerifyBlock) return lds.token;
-        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kSumSlots; ++t) {
+            const long long j = j0 + (t * 64 + lane) * EPV;
+            if (j0 + (long long)t * 64 * EPV >= to) break;
+            float z[EPV];
+            double ep[EPV];
+            unpack<DT>(zr[t], z);
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) {
+                ep[e] = exp_from(z[e], pk, r.k);
+                s[0] += ep[e];
+            }
+            if (r.d) {
+                unpack<DT>(dr[t], z);
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) {
+                    const double eq = exp_from(z[e], r.qk, r.kd);
+                    s[1] += eq;
+                    const double w = fma(-r.rho, eq, ep[e]);
+                    if constexpr (EXACT) {
+                        s[2] += fmax(w, 0.0);
+                    } else {
+                        s[2] += w > 0.0 ? ep[e] : 0.0;
+                        s[3] += w > 0.0 ? eq : 0.0;
+                        s[4] += fabs(w) <= kNearSide * ep[e] ? ep[e] : 0.0;
+                    }
+                }
+            } else if (r.y >= 0) {
+#pragma unroll
+                for (int e = 0; e < EPV; ++e) s[2] += j + e == r.y ? 0.0 : ep[e];
+            }
+        }
     }
-    // the part's entries, added up in another order, stay below what its sum promised: the last that has any
-    atomicMax(&lds.last, fallback);
-    __syncthreads();
-    return from + lds.last;
+    if (!max_known) top = m;
+    s[0] = wave_sum_dpp(s[0]);
+    if (!(top < INFINITY)) s[0] = __builtin_nan("");
+    if (r.d) {
+        s[1] = wave_sum_dpp(s[1]);
+        s[3] = wave_sum_dpp(s[3]);
+        s[4] = wave_sum_dpp(s[4]);
+    }
+    if (r.d || r.y >= 0) s[2] = wave_sum_dpp(s[2]);
+}
+
+template <grpo_dtype DT>
+__global__ void __launch_bounds__(kVerifyBlock) verify_sums_k(Verify p)
+{
+    __shared__ Position at[kMaxDrafts];
+    __shared__ double whole[kVerifyBlock / 64][2];
+    const int b = blockIdx.x / p.sum_blocks, c = blockIdx.x % p.sum_blocks;
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int len = p.length(b);
+    if (len < 0) return;
+    for (int i = wave; i < len; i += kVerifyBlock / 64) {
+        const Position r = position<DT>(p, b, i);
+        if ((tid & 63) == 0) at[i] = r;
+    }
+    if (len > 0) __syncthreads();
+    Weights r = {};
+    r.k = p.k;
+    r.kd = p.kd;
+    r.y = -1;
+    double s[kSums];
+    float top = -INFINITY;
+    int n = 0;
+    for (; n < len; ++n) {
+        const float u = p.u[(long long)b * p.drafts + n];
+        int said = verdict(u, at[n]);
+        if (said == kNear) {  // by the whole rows' sums in fp64, a quarter of them to a wavefront
+            const long long y = p.tokens[(long long)b * p.drafts + n], quarter = (p.vocab / 4 + 7) / 8 * 8, from = wave * quarter;
+            r.t = p.target_row(b, n);
+            r.d = p.draft ? p.draft_row(b, n) : nullptr;
+            r.pk = times_k(at[n].p.max, p.k);
+            r.qk = times_k(at[n].q.max, p.kd);
+            top = at[n].p.max;
+            part_sums<DT>(r, from, wave < 3 && from + quarter < p.vocab ? from + quarter : p.vocab, true, top, s);
+            __syncthreads();
+            if ((tid & 63) == 0) {
+                whole[wave][0] = s[0];
+                whole[wave][1] = s[1];
+            }
+            __syncthreads();
+            const double sp = whole[0][0] + whole[1][0] + whole[2][0] + whole[3][0], sq = whole[0][1] + whole[1][1] + whole[2][1] + whole[3][1];
+            const double py = exp_from(load_elem<DT>(r.t, y), r.pk, p.k) / sp;
+            const double qy = r.d ? exp_from(load_elem<DT>(r.d, y), r.qk, p.kd) / sq : 1.0;
+            said = (double)u * qy < py ? kAccepted : kRefused;
+        }
+        if (said == kRefused) break;
+    }
+    const bool refused = n < len;
+    r.t = p.target_row(b, n);
+    r.d = nullptr;
+    top = -INFINITY;
+    if (refused) {
+        top = at[n].p.max;
+        r.pk = times_k(top, p.k);
+        if (p.draft) {
+            r.d = p.draft_row(b, n);
+            r.qk = times_k(at[n].q.max, p.kd);
+            r.rho = at[n].p.sum / at[n].q.sum;
+        } else {
+            r.y = p.tokens[(long long)b * p.drafts + n];
+        }
+    }
+    const int piece = c * (kVerifyBlock / 64) + wave;
+    if (piece < p.pieces) {
+        const long long from = (long long)piece * p.piece, to = from + p.piece < p.vocab ? from + p.piece : p.vocab;
+        part_sums<DT>(r, from, to, refused, top, s);
+        if ((tid & 63) == 0) {
+            double *sums = p.sums + ((long long)b * p.pieces + piece) * kSums;
+#pragma unroll
+            for (int i = 0; i < kSums; ++i) sums[i] = s[i];
+            p.tops[(long long)b * p.pieces + piece] = top;
+        }
+    }
+    if (c != 0) return;
+    if (tid == 0) {
+        p.refusal[b] = {n, refused, refused ? at[n].p.max : 0.f, refused ? at[n].q.max : 0.f, r.rho};
+        p.accepted_out[b] = n;
+    }
+    if (tid < n) {
+        p.tokens_out[(long long)b * (p.drafts + 1) + tid] = p.tokens[(long long)b * p.drafts + tid];
+        p.logprobs_out[(long long)b * (p.drafts + 1) + tid] = (float)log(at[tid].py);
+    }
+}
+
+// Which piece of row n holds the token, by one wavefront, each lane with its share of the pieces, neighbours.
+struct Found {
+    int piece;             // -1: there is no token, -2: the sums have to be formed again, with rho as it is here
+    double base, target;   // the sum in front of the piece, and the one to cross
+    double total;          // S_p
+    double pk, rho;
+    int whole;             // w is p after all: nothing is left of p - q
+};
+__device__ __forceinline__ Found find_piece(const Verify &p, int b, const Refusal &at, const Weights &r, bool exact)
+{
+    const int lane = threadIdx.x & 63;
+    const int share = (p.pieces + 63) / 64, first = lane * share, end = first + share < p.pieces ? first + share : p.pieces;
+    const double *sums = p.sums + (long long)b * p.pieces * kSums;
+    const float *tops = p.tops + (long long)b * p.pieces;
+    Found f = {-1, 0.0, 0.0, 0.0, 0.0, 0.0, 0};
+    float top = at.max_p;
+    if (!at.refused) {  // each piece's sum is relative to its own maximum
+        top = -INFINITY;
+        for (int i = first; i < end; ++i) top = maximum(top, tops[i]);
+        top = wave_maximum(top);
+    }
+    f.pk = times_k(top, p.k);
+    auto of_p = [&](int i) { return at.refused ? sums[kSums * i] : sums[kSums * i] * exp_from(tops[i], f.pk, p.k); };
+    double sp = 0.0, sq = 0.0;
+    for (int i = first; i < end; ++i) {
+        sp += of_p(i);
+        if (r.d) sq += sums[kSums * i + 1];
+    }
+    const double front = wave_scan(sp);
+    f.total = last_lane(front);
+    if (r.d) sq = wave_sum_dpp(sq);
+    if (!(f.total > 0.0 && top < INFINITY) || (r.d && !(sq > 0.0 && at.max_q < INFINITY))) return f;  // NaN too
+    double w = sp, up = front, all = f.total;
+    bool whole = !r.d && r.y < 0;
+    if (!whole) {
+        f.rho = r.d ? f.total / sq : 0.0;
+        w = 0.0;
+        for (int i = first; i < end; ++i) w += fmax(fma(-f.rho, sums[kSums * i + 3], sums[kSums * i + 2]), 0.0);
+        up = wave_scan(w);
+        all = last_lane(up);
+        if (r.d && !exact) {
+            double near = 0.0;
+            for (int i = first; i < end; ++i) near += sums[kSums * i + 4];
+            near = wave_sum_dpp(near);
+            const double off = fabs(f.rho - at.rho) / f.rho;
+            if (!(off <= kNearSide && off * near <= 0x1p-38 * all && all >= 0x1p-10 * f.total)) {
+                f.piece = -2;
+                return f;
+            }
+        }
+        if (!(all > 0.0)) {
+            f.whole = 1;
+            whole = true;
+            w = sp;
+            up = front;
+            all = f.total;
+        }
+    }
+    f.target = p.v[b] * all;
+    // the first lane whose pieces cross, or, where the number is next to 1 and rounding keeps the sum, the last that has any
+    const unsigned long long cross = __ballot(up > f.target), any = __ballot(w > 0.0);
+    const int owner = cross ? __builtin_ctzll(cross) : 63 - __builtin_clzll(any);
+    double run = up - w;
+    int piece = -1;
+    double base = run;
+    if (lane == owner)
+        for (int i = first; i < end; ++i) {
+            const double x = whole ? of_p(i) : fmax(fma(-f.rho, sums[kSums * i + 3], sums[kSums * i + 2]), 0.0);
+            if (x > 0.0) {
+                piece = i;
+                base = run;
+            }
+            run += x;
+            if (run > f.target) break;
+        }
+    f.piece = __shfl(piece, owner, 64);
+    f.base = __shfl(base, owner, 64);
+    return f;
 }
 
 template <grpo_dtype DT>
 __global__ void __launch_bounds__(kVerifyBlock) verify_pick_k(Verify p)
 {
     constexpr int EPV = Elem<DT>::EPV;
-    __shared__ double ratio_p[kMaxDrafts], ratio_q[kMaxDrafts];
-    __shared__ RowSum row_p[kMaxDrafts + 1], row_q[kMaxDrafts];
-    __shared__ PickLds lds;
-    __shared__ bool last_one;
-    const int b = blockIdx.x / p.pickers, c = blockIdx.x % p.pickers;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int len = p.length(b);
+    __shared__ Found lds_found;
+    __shared__ double lds_wave[2][kVerifyBlock / 64];
+    __shared__ int lds_first[2], lds_last;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int K = p.drafts;
     long long *tokens_out = p.tokens_out + (long long)b * (K + 1);
     float *logprobs_out = p.logprobs_out + (long long)b * (K + 1);
-    if (len < 0) {  // not a response
-        if (c == 0) {
-            for (int i = tid; i <= K; i += kVerifyBlock) {
-                tokens_out[i] = -1;
-                logprobs_out[i] = 0.f;
+    const bool response = p.length(b) >= 0;
+    const Refusal at = response ? p.refusal[b] : Refusal{-1, 0, 0.f, 0.f, 0.0};
+    if (tid <= K && tid > at.n) {  // (a response that is none has no place n)
+        tokens_out[tid] = -1;
+        logprobs_out[tid] = 0.f;
+    }
+    if (!response) {
+        if (tid == 0) p.accepted_out[b] = 0;
+        return;
+    }
+    Weights r = {};
+    r.k = p.k;
+    r.kd = p.kd;
+    r.y = -1;
+    r.t = p.target_row(b, at.n);
+    if (at.refused && p.draft) {
+        r.d = p.draft_row(b, at.n);
+        r.qk = times_k(at.max_q, p.kd);
+    } else if (at.refused) {
+        r.y = p.tokens[(long long)b * K + at.n];
+    }
+    if (wave == 0) {
+        const Found f = find_piece(p, b, at, r, false);
+        if (lane == 0) {
+            lds_found = f;
+            lds_first[0] = lds_first[1] = 0x7fffffff;
+            lds_last = -1;
+        }
+    }
+    __syncthreads();
+    if (lds_found.piece == -2) {
+        r.pk = lds_found.pk;
+        r.rho = lds_found.rho;
+        for (int i = wave; i < p.pieces; i += kVerifyBlock / 64) {
+            const long long from = (long long)i * p.piece, to = from + p.piece < p.vocab ? from + p.piece : p.vocab;
+            double s[kSums];
+            float top = at.max_p;
+            part_sums<DT, true>(r, from, to, true, top, s);
+            if (lane == 0) {
+                p.sums[((long long)b * p.pieces + i) * kSums + 2] = s[2];
+                p.sums[((long long)b * p.pieces + i) * kSums + 3] = 0.0;
             }
-            if (tid == 0) p.accepted_out[b] = 0;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            const Found f = find_piece(p, b, at, r, true);
+            if (lane == 0) lds_found = f;
+        }
+        __syncthreads();
+    }
+    const Found f = lds_found;
+    if (f.piece < 0) {
+        if (tid == 0) {
+            tokens_out[at.n] = -1;
+            logprobs_out[at.n] = __builtin_nanf("");
         }
         return;
     }
-    for (int i = wave; i <= len; i += kVerifyBlock / 64) {
-        const RowSum rp = row_sum(p.parts(b, i), p.chunks, p.k);
-        RowSum rq = {1.0, 0.f};
-        if (p.draft && i < len) rq = row_sum(p.parts(b, K + 1 + i), p.chunks, p.kd);
-        if (lane == 0) {
-            row_p[i] = rp;
-            if (i < len) {
-                row_q[i] = rq;
-                const long long y = p.tokens[(long long)b * K + i];
-                const bool in = y >= 0 && y < p.vocab;
-                ratio_p[i] = in ? exp_from(load_elem<DT>(p.target_row(b, i), y), rp.max, p.k) / rp.sum : 0.0;
-                ratio_q[i] = !p.draft ? 1.0 : in ? exp_from(load_elem<DT>(p.draft_row(b, i), y), rq.max, p.kd) / rq.sum : 0.0;
-            }
-        }
+    if (f.whole) {
+        r.d = nullptr;
+        r.y = -1;
     }
-    __syncthreads();
-    int n = 0;
-    while (n < len && (double)p.u[(long long)b * K + n] * ratio_q[n] < ratio_p[n]) ++n;
-    if (c == 0) {
-        for (int i = tid; i <= K; i += kVerifyBlock) {
-            if (i < n) {
-                tokens_out[i] = p.tokens[(long long)b * K + i];
-                logprobs_out[i] = (float)log(ratio_p[i]);
-            } else if (i > n) {
-                tokens_out[i] = -1;
-                logprobs_out[i] = 0.f;
-            }
-        }
-        if (tid == 0) p.accepted_out[b] = n;
-    }
-    Residual r = {};
-    r.t = p.target_row(b, n);
-    r.y = -1;
-    r.k = p.k;
-    r.kd = p.kd;
-    r.mp = row_p[n].max;
-    r.inv_sp = 1.0;
-    bool residual = n < len;
-    if (residual) {
-        r.inv_sp = 1.0 / row_p[n].sum;
-        if (p.draft) {
-            r.d = p.draft_row(b, n);
-            r.mq = row_q[n].max;
-            r.inv_sq = 1.0 / row_q[n].sum;
-        } else {
-            r.y = p.tokens[(long long)b * K + n];
-        }
-        const long long from = (long long)c * p.chunk, to = from + p.chunk < p.vocab ? from + p.chunk : p.vocab;
-        double s = 0.0;
-        for (long long j = from + tid * EPV; j < to; j += kVerifyBlock * EPV) {
-            double w[EPV];
-            weights<DT>(r, j, to, w);
-#pragma unroll
-            for (int e = 0; e < EPV; ++e) s += w[e];
-        }
-        s = wave_sum_dpp(s);
-        if (lane == 0) lds.wave[wave] = s;
-        __syncthreads();
-        if (tid == 0) {
-            s = 0.0;
-#pragma unroll
-            for (int i = 0; i < kVerifyBlock / 64; ++i) s += lds.wave[i];
-            p.w[(long long)b * p.chunks + c] = s;
-            __threadfence();
-            last_one = atomicAdd(&p.ticket[b], 1u) == (unsigned)p.chunks - 1;
-        }
-        __syncthreads();
-        if (!last_one) return;
-        __threadfence();
-        for (int i = tid; i < p.chunks; i += kVerifyBlock) lds.prefix[i] = p.w[(long long)b * p.chunks + i];
-    } else {
-        if (c != 0) return;
-    }
+    r.pk = f.pk;
+    r.rho = f.rho;
+    const long long from = (long long)f.piece * p.piece, to = from + p.piece < p.vocab ? from + p.piece : p.vocab;
+    double base = f.base;
+    int last = -1, turn = 0;  // this lane's last entry that has a weight
     long long token = -1;
-    __syncthreads();
-    for (int pass = residual ? 0 : 1; pass < 2; ++pass) {
-        if (pass == 1) {
-            // behind the last draft, or with nothing left of p - q but rounding: from p itself
-            r.d = nullptr;
-            r.y = -1;
-            r.inv_sp = 1.0;
-            const VerifyPart *part = p.parts(b, n);
-            for (int i = tid; i < p.chunks; i += kVerifyBlock)
-                lds.prefix[i] = part[i].sum * exp_from(part[i].max, finite_max(r.mp), p.k);
+    for (long long j0 = from; j0 < to; j0 += kVerifyBlock * EPV, turn ^= 1) {
+        const long long j = j0 + tid * EPV;
+        double w[EPV], sum = 0.0;
+        weights<DT>(r, j, to, w);
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) {
+            sum += w[e];
+            if (w[e] > 0.0) last = (int)(j - from) + e;
+        }
+        const double up = wave_scan(sum);
+        if (lane == 63) lds_wave[turn][wave] = up;
+        __syncthreads();
+        double before = base;
+#pragma unroll
+        for (int i = 0; i < kVerifyBlock / 64; ++i) {
+            if (i < wave) before += lds_wave[turn][i];
+            base += lds_wave[turn][i];
+        }
+        const unsigned long long cross = __ballot(before + up > f.target);
+        if (cross && before <= f.target && lane == (int)__builtin_ctzll(cross)) {  // the first lane of the wavefront whose entries cross; one of them does, up to rounding
+            int first = last;
+            double run = before + (up - sum);
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) {
+                if (run <= f.target && w[e] > 0.0) first = (int)(j - from) + e;
+                run += w[e];
+            }
+            atomicMin(&lds_first[turn], first);
         }
         __syncthreads();
-        token = pick_token<DT>(p, r, p.v[b], lds);
-        const bool nothing = lds.prefix[p.chunks - 1] == 0.0;
+        if (lds_first[turn] != 0x7fffffff) {
+            token = from + lds_first[turn];
+            break;
+        }
+    }
+    if (token < 0) {  // the entries, added up in another order, stay below what the piece's sum promised: the last that has any
+        atomicMax(&lds_last, last);
         __syncthreads();
-        if (!nothing) break;
+        token = from + lds_last;
     }
     if (tid == 0) {
-        tokens_out[n] = token;
-        logprobs_out[n] = token < 0 ? __builtin_nanf("")
-                                    : (float)(((double)load_elem<DT>(r.t, token) - (double)r.mp) * p.inv_t - log(row_p[n].sum));
+        tokens_out[at.n] = token;
+        logprobs_out[at.n] = (float)(fma((double)load_elem<DT>(r.t, token), p.k, -f.pk) * 0.6931471805599453094 - log(f.total));
     }
 }
 
-// Entries in a part of a row, and parts.  Enough parts that all rows' fill the GPU, and no more than pick_token has room for.
-static bool verify_plan(int64_t batch, int64_t drafts, int64_t vocab, int dtype, int *chunk, int *chunks)
+// Entries in a part of a row, and parts: at least `enough` workgroups of kVerifyBlock where the rows are long enough for it, `most` parts
+// at most.
+static bool verify_cut(int64_t rows, int64_t vocab, int dtype, int64_t enough, int64_t most, int *chunk, int *chunks)
 {
-    if (batch < 0 || batch > 0x7fffffffll || drafts < 0 || drafts > kMaxDrafts || vocab <= 0 || vocab > kMaxVocab) return false;
-    const int64_t rows = batch * (2 * drafts + 1);
     const int64_t unit = kVerifyBlock * (dtype == GRPO_BF16 ? 8 : 4);
     int64_t units = 1;
-    while ((vocab + units * unit - 1) / (units * unit) > kMaxChunks) units *= 2;
-    while (units < kVerifySlots && rows * ((vocab + unit * units - 1) / (unit * units)) >= 4096) units *= 2;
+    while ((vocab + units * unit - 1) / (units * unit) > most) units *= 2;
+    while (units < kVerifySlots && rows * ((vocab + unit * units - 1) / (unit * units)) >= enough) units *= 2;
     *chunk = (int)(units * unit);
     *chunks = (int)((vocab + units * unit - 1) / (units * unit));
     return rows * *chunks <= 0x7fffffffll;  // workgroups
+}
+
+// The parts, and where they lie in the workspace; its size, or 0 for sizes that cannot be.
+static size_t verify_plan(Verify &p, int64_t batch, int64_t drafts, int64_t vocab, int dtype, uintptr_t ws)
+{
+    if ((dtype != GRPO_F32 && dtype != GRPO_BF16) || batch < 0 || batch > 0x7fffffffll || drafts < 0 || drafts > kMaxDrafts || vocab <= 0 ||
+        vocab > kMaxVocab)
+        return 0;
+    int sum_chunk;
+    if (!verify_cut(batch * 2 * drafts, vocab, dtype, kRowsEnough, kMaxChunks, &p.chunk, &p.chunks) ||
+        !verify_cut(batch, vocab, dtype, kSumsEnough, kMaxChunks / 4, &sum_chunk, &p.sum_blocks))
+        return 0;
+    p.piece = sum_chunk / (kVerifyBlock / 64);
+    p.pieces = (int)((vocab + p.piece - 1) / p.piece);
+    const uintptr_t begin = ws;
+    p.part = (unsigned long long *)ws;
+    ws += align_up((size_t)batch * 2 * drafts * p.chunks * 8, 256);
+    p.sums = (double *)ws;
+    ws += align_up((size_t)batch * p.pieces * kSums * 8, 256);
+    p.tops = (float *)ws;
+    ws += align_up((size_t)batch * p.pieces * 4, 256);
+    p.refusal = (Refusal *)ws;
+    ws += align_up((size_t)batch * sizeof(Refusal) + 1, 256);
+    return ws - begin;
 }
 
 }  // namespace grpo_impl
@@ -440,11 +727,8 @@ extern "C" {
 
 size_t grpo_verify_workspace_bytes(int64_t batch, int64_t drafts, int64_t vocab, grpo_dtype dtype_arg)
 {
-    const int dtype = raw_enum(dtype_arg);
-    int chunk, chunks;
-    if ((dtype != GRPO_F32 && dtype != GRPO_BF16) || !verify_plan(batch, drafts, vocab, dtype, &chunk, &chunks)) return 0;
-    return align_up((size_t)batch * 4 + 1, 256) + align_up((size_t)batch * chunks * 8, 256) +
-           (size_t)batch * (2 * drafts + 1) * chunks * sizeof(VerifyPart);
+    Verify p;
+    return verify_plan(p, batch, drafts, vocab, raw_enum(dtype_arg), 0);
 }
 
 grpo_status grpo_verify_drafts(const void *target_logits, int64_t target_batch_stride, int64_t target_row_stride, const void *draft_logits,
@@ -456,8 +740,10 @@ grpo_status grpo_verify_drafts(const void *target_logits, int64_t target_batch_s
     const int dtype = raw_enum(dtype_arg);
     if (dtype != GRPO_F32 && dtype != GRPO_BF16) return GRPO_ERR_DTYPE;
     Verify p = {};
-    if (!verify_plan(batch, drafts, vocab, dtype, &p.chunk, &p.chunks)) return GRPO_ERR_SHAPE;
-    if (!(temperature > 0.0) || !std::isfinite(temperature) || !(draft_temperature > 0.0) || !std::isfinite(draft_temperature)) return GRPO_ERR_PARAM;
+    const size_t need = verify_plan(p, batch, drafts, vocab, dtype, (uintptr_t)workspace);
+    if (need == 0) return GRPO_ERR_SHAPE;
+    // 1 / T has to be a number in fp32 too
+    if (!(temperature >= 1e-30 && temperature <= 1e30) || !(draft_temperature >= 1e-30 && draft_temperature <= 1e30)) return GRPO_ERR_PARAM;
     if (batch == 0) return GRPO_OK;
     if (!target_logits || !sample_u || !tokens_out || !n_accepted_out || !logprobs_out) return GRPO_ERR_NULL;
     if (drafts > 0 && (!draft_tokens || !accept_u)) return GRPO_ERR_NULL;
@@ -468,7 +754,7 @@ grpo_status grpo_verify_drafts(const void *target_logits, int64_t target_batch_s
     if (((uintptr_t)target_logits & 15u) || ((target_row_stride * bytes) & 15) || ((target_batch_stride * bytes) & 15)) return GRPO_ERR_ALIGN;
     if (draft_logits && (((uintptr_t)draft_logits & 15u) || ((draft_row_stride * bytes) & 15) || ((draft_batch_stride * bytes) & 15)))
         return GRPO_ERR_ALIGN;
-    if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < grpo_verify_workspace_bytes(batch, drafts, vocab, dtype_arg))
+    if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)
         return GRPO_ERR_WORKSPACE;
     p.target = (const char *)target_logits;
     p.tb = target_batch_stride * bytes;
@@ -484,28 +770,21 @@ grpo_status grpo_verify_drafts(const void *target_logits, int64_t target_batch_s
     p.drafts = (int)drafts;
     p.vocab = vocab;
     const double log2e = 1.4426950408889634074;
-    p.inv_t = 1.0 / temperature;
     p.k = log2e / temperature;
     p.kd = log2e / draft_temperature;
-    char *ws = (char *)workspace;
-    p.ticket = (unsigned *)ws;
-    ws += align_up((size_t)batch * 4 + 1, 256);
-    p.w = (double *)ws;
-    ws += align_up((size_t)batch * p.chunks * 8, 256);
-    p.part = (VerifyPart *)ws;
     p.tokens_out = (long long *)tokens_out;
     p.accepted_out = n_accepted_out;
     p.logprobs_out = logprobs_out;
     hipStream_t st = (hipStream_t)stream;
-    const unsigned row_blocks = (unsigned)(batch * (draft_logits ? 2 * drafts + 1 : drafts + 1) * p.chunks);
-    p.pickers = drafts > 0 ? p.chunks : 1;
-    const unsigned pick_blocks = (unsigned)(batch * p.pickers);
+    const unsigned row_blocks = (unsigned)(batch * drafts * (draft_logits ? 2 : 1) * p.chunks), sum_blocks = (unsigned)(batch * p.sum_blocks);
     if (dtype == GRPO_BF16) {
-        hipLaunchKernelGGL(verify_rows_k<GRPO_BF16>, dim3(row_blocks), dim3(kVerifyBlock), 0, st, p);
-        hipLaunchKernelGGL(verify_pick_k<GRPO_BF16>, dim3(pick_blocks), dim3(kVerifyBlock), 0, st, p);
+        if (row_blocks > 0) hipLaunchKernelGGL(verify_rows_k<GRPO_BF16>, dim3(row_blocks), dim3(kVerifyBlock), 0, st, p);
+        hipLaunchKernelGGL(verify_sums_k<GRPO_BF16>, dim3(sum_blocks), dim3(kVerifyBlock), 0, st, p);
+        hipLaunchKernelGGL(verify_pick_k<GRPO_BF16>, dim3((unsigned)batch), dim3(kVerifyBlock), 0, st, p);
     } else {
-        hipLaunchKernelGGL(verify_rows_k<GRPO_F32>, dim3(row_blocks), dim3(kVerifyBlock), 0, st, p);
-        hipLaunchKernelGGL(verify_pick_k<GRPO_F32>, dim3(pick_blocks), dim3(kVerifyBlock), 0, st, p);
+        if (row_blocks > 0) hipLaunchKernelGGL(verify_rows_k<GRPO_F32>, dim3(row_blocks), dim3(kVerifyBlock), 0, st, p);
+        hipLaunchKernelGGL(verify_sums_k<GRPO_F32>, dim3(sum_blocks), dim3(kVerifyBlock), 0, st, p);
+        hipLaunchKernelGGL(verify_pick_k<GRPO_F32>, dim3((unsigned)batch), dim3(kVerifyBlock), 0, st, p);
     }
     return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
 }

@@ -1,8 +1,10 @@
 """Verification of drafted tokens against its definition, one response after the other in fp64 on the CPU.
 
-Tokens and counts are compared as they are: both sides form probabilities and sums in fp64, which agree to about 1e-13, so that a
-random number would have to lie within that of a border.  Log-probs are rounded to fp32 once, 2^-24 of their value; 1e-9 covers
-what fp64 loses in front of that."""
+Tokens and counts are compared as they are: what decides them is formed in fp64 on both sides, and agrees to about 1e-12, so that a
+random number would have to lie within that of a border.  The sampled token's log-prob is rounded to fp32 once, 2^-24 of its value;
+1e-9 covers what fp64 loses in front of that.  Those of accepted drafts come from fp32 sums: a term 2^x of one is off by 2^-23 and by
+the roundings of z - m, of 1 / T and of x, 0.7 |x| 2^-24 each, where |x| <= 40 (smaller terms make up less than 2^-22 of a sum of
+2^18), and by four roundings in sums: 94 * 2^-24 < 2^-17."""
 import numpy as np
 import pytest
 import torch
@@ -65,7 +67,8 @@ def check(target, draft, tokens, u, v, lengths=None, t=1.0, td=1.0):
     lp = got[2].cpu().double().numpy()
     assert np.array_equal(np.isnan(lp), np.isnan(lps))
     off = np.abs(np.nan_to_num(lp) - np.nan_to_num(lps))
-    assert (off <= 2.0 ** -24 * np.abs(np.nan_to_num(lps)) + 1e-9).all(), off.max()
+    accepted = np.arange(lp.shape[1]) < acc[:, None]
+    assert (off <= 2.0 ** -24 * np.abs(np.nan_to_num(lps)) + np.where(accepted, 2.0 ** -17, 1e-9)).all(), off.max()
     return got
 
 
@@ -166,6 +169,45 @@ def test_ratios_at_their_borders():
     got = check(rows(target, F32), rows(q[:, None], F32), tokens, u, v)
     # 0.5 * 0.5 is not below 0.25; p = q = 0 is not accepted; p > 0 = q always is; p = 0 never
     assert got[1].tolist() == [0, 1, 0, 1, 0]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("vocab", [5, 700, 9001, 152064])
+def test_random_numbers_next_to_the_ratio(vocab, dtype):
+    """Ratios that are within a few steps of fp32 of their random number: fp32 sums cannot tell on which side."""
+    n = 24 if vocab < 100000 else 6
+    target, draft, tokens, u, v = make(vocab, n, 2, vocab, dtype)
+    t, d = target.float().cpu().numpy(), draft.float().cpu().numpy()
+    for b in range(n):
+        for i in range(2):
+            p, q = softmax(t[b, i], 1.0), softmax(d[b, i], 1.0)
+            y = next(y for y in np.argsort(-q) if p[y] < q[y])
+            tokens[b, i] = int(y)
+            x = np.float32(p[y] / q[y])
+            for _ in range(b % 3):
+                x = np.nextafter(x, np.float32(b % 2 * 2))
+            u[b, i] = float(x)
+    got = check(target, draft, tokens, u, v)
+    if vocab > 5:
+        assert 0 < got[1].double().mean() < 2
+
+
+@pytest.mark.parametrize("vocab", [50, 5003, 152064])
+def test_drafts_from_nearly_the_same_logits(vocab):
+    """Logits that differ in a few places only: what is left of p - q is little, most of it the difference of the sums, and for
+    most of the entries p / q is one and the same number next to 1, on a side that fp32 sums do not tell."""
+    n = 40 if vocab < 100000 else 8
+    target, draft, tokens, u, v = make(vocab, n, 1, vocab, F32, near=0.0)
+    g = torch.Generator().manual_seed(vocab)
+    for b in range(n):
+        j = torch.randint(0, vocab, (1 + b % 3,), generator=g).cuda()
+        draft[b, 0, j] += 4.0 * 10.0 ** -(b % 7)  # the draft likes a few tokens more: all others are likelier under p
+        if b % 2:
+            draft[b, 0, (j + 1) % vocab] -= 3.0 * 10.0 ** -(b % 5)
+        tokens[b, 0] = int(j[0])
+    u[:] = 1 - 2.0 ** -24
+    got = check(target, draft, tokens, u, v)
+    assert (got[1] == 0).double().mean() > 0.9  # (where a place was raised and lowered, p may be the larger one)
 
 
 def test_the_same_distributions():

@@ -26,7 +26,7 @@ VERIFY = dict(target=P, tb=4096, ts=1024, draft=P, db=4096, ds=1024, dtype=1, n=
     (dict(dtype=2), DTYPE), (dict(dtype=-1), DTYPE),
     (dict(n=-1), SHAPE), (dict(n=1 << 31), SHAPE), (dict(n=1 << 30), SHAPE), (dict(k=-1), SHAPE), (dict(k=65), SHAPE), (dict(V=0), SHAPE),
     (dict(V=(1 << 28) + 1), SHAPE), (dict(ts=992), SHAPE), (dict(ds=992), SHAPE), (dict(tb=-8), SHAPE), (dict(db=-8), SHAPE),
-    (dict(t=0.0), PARAM), (dict(t=-1.0), PARAM), (dict(t=NAN), PARAM), (dict(t=INF), PARAM), (dict(td=0.0), PARAM), (dict(td=NAN), PARAM),
+    (dict(t=0.0), PARAM), (dict(t=-1.0), PARAM), (dict(t=NAN), PARAM), (dict(t=INF), PARAM), (dict(t=1e-31), PARAM), (dict(td=1e31), PARAM), (dict(td=0.0), PARAM), (dict(td=NAN), PARAM),
     (dict(target=None), NULL), (dict(tokens=None), NULL), (dict(u=None), NULL), (dict(v=None), NULL), (dict(out=None), NULL),
     (dict(acc=None), NULL), (dict(lp=None), NULL),
     (dict(target=P + 8), ALIGN), (dict(ts=1001), ALIGN), (dict(tb=4097), ALIGN), (dict(draft=P + 4), ALIGN), (dict(ds=1004), ALIGN),
@@ -46,8 +46,8 @@ def test_verify_workspace():
     for n, k, v in ((0, 0, 1), (1, 0, 1), (1, 64, 1 << 28), (96, 5, 152064), (1000, 8, 300007), (1 << 20, 0, 1000)):
         for dtype in (0, 1):
             need = f(n, k, v, dtype)
-            # a sum and a maximum to each part of a row, at most 1024 parts
-            assert 0 < need <= 512 + n * (4 + 1024 * 8 + (2 * k + 1) * 1024 * 16 + 512)
+            # sums to each part of a row, at most 1024 parts
+            assert 0 < need <= 1024 + n * (k + 2) * 4 + n * 1024 * (2 * k * 8 + 44)
             a = dict(VERIFY, n=n, k=k, V=v, dtype=dtype, ts=(v + 7) // 8 * 8, ds=(v + 7) // 8 * 8, bytes=need - 1)
             if n:
                 assert grpo.lib().grpo_verify_drafts(*a.values()) == WORKSPACE
