@@ -143,14 +143,17 @@ def _load_lib():
     L.grpo_grad_norm_workspace_bytes.restype = sz
     L.grpo_grad_norm_workspace_bytes.argtypes = []
     L.grpo_grad_norm.restype = i32
-    L.grpo_grad_norm.argtypes = [ctypes.POINTER(_OptimPlan), vp, f64, vp, vp, sz, vp]
+    L.grpo_grad_norm.argtypes = [vp, vp, f64, vp, vp, sz, vp]
     L.grpo_adamw_step.restype = i32
-    L.grpo_adamw_step.argtypes = [ctypes.POINTER(_OptimPlan), vp, i64, vp, f64, vp, f64, f64, f64, vp, vp]
+    L.grpo_adamw_step.argtypes = [vp, vp, i64, vp, f64, vp, f64, f64, f64, vp, vp]
     fast = _load_fastcall()
     if fast is not None:
         fast.bind(*[ctypes.cast(f, vp).value for f in (
             L.grpo_workspace_bytes, L.grpo_group_advantages, L.grpo_logprobs_fwd, L.grpo_loss_fwd_bwd,
             L.grpo_loss_aux_fwd_bwd, L.grpo_total_rewards, L.grpo_filter_groups, L.grpo_packed_layout)])
+        fast.bind_operators(*[ctypes.cast(f, vp).value for f in (
+            L.grpo_verify_workspace_bytes, L.grpo_verify_drafts, L.grpo_block_norm_workspace_bytes, L.grpo_block_norm_fwd,
+            L.grpo_block_norm_bwd, L.grpo_grad_norm_workspace_bytes, L.grpo_grad_norm, L.grpo_adamw_step)])
         _fast = fast
     _lib = L
 
@@ -684,6 +687,17 @@ def grpo_lmhead_loss_aux_fwd_bwd(hidden, weight, tokens, old_logprobs, ref_logpr
     return loss_out, logprobs_out, entropy_out, counts_out, grad_hidden, grad_weight
 
 
+def _call(where, device, f, *args):
+    """Calls the library on a tensor's device, whichever is the current one."""
+    if device.index == torch.cuda.current_device():
+        rc = f(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = f(*args)
+    if rc != GRPO_OK:
+        raise GrpoError(rc, where)
+
+
 def _verify_logits(t, name, batch, rows, vocab, dtype, device):
     """The strides of responses and of rows of [batch, rows, vocab] logits, in elements."""
     if t.dim() != 3 or t.dtype != dtype or tuple(t.shape) != (batch, rows, vocab) or (t.stride(2) != 1 and vocab > 1):
@@ -710,6 +724,10 @@ def grpo_verify_drafts(target_logits, draft_logits, draft_tokens, accept_u, samp
     tokens that no model drafted; draft_tokens [batch, drafts] i64 and accept_u [batch, drafts] f32 (either may be None without
     drafts); sample_u [batch] f64; draft_lengths [batch] i32 or None.  Returns (tokens [batch, drafts + 1] i64,
     n_accepted [batch] i32, logprobs [batch, drafts + 1] f32)."""
+    if tokens_out is None and n_accepted_out is None and logprobs_out is None and workspace is None and stream is None:
+        out = _fast.verify_drafts(target_logits, draft_logits, draft_tokens, accept_u, sample_u, draft_lengths, temperature, draft_temperature)
+        if out is not None:
+            return _fast_result(out, "grpo_verify_drafts")
     if not target_logits.is_cuda:
         raise ValueError("target_logits must be a device tensor: libgrpo has no CPU path")
     if target_logits.dim() != 3 or target_logits.dtype not in _DTYPE_CODES or target_logits.shape[1] < 1:
@@ -745,11 +763,9 @@ def grpo_verify_drafts(target_logits, draft_logits, draft_tokens, accept_u, samp
     L, code = lib(), _DTYPE_CODES[dtype]
     if workspace is None:
         workspace = torch.empty(L.grpo_verify_workspace_bytes(n, k, v, code), dtype=torch.uint8, device=dev)
-    rc = L.grpo_verify_drafts(_ptr(target_logits), tb, tk, _ptr(draft_logits), db, dk, code, n, k, v, _ptr(draft_tokens), _ptr(accept_u),
-                              _ptr(sample_u), _ptr(draft_lengths), float(temperature), float(draft_temperature), _ptr(tokens_out),
-                              _ptr(n_accepted_out), _ptr(logprobs_out), _ptr(workspace), workspace.numel(), _raw_stream(stream, dev.index))
-    if rc != GRPO_OK:
-        raise GrpoError(rc, "grpo_verify_drafts")
+    _call("grpo_verify_drafts", dev, L.grpo_verify_drafts, _ptr(target_logits), tb, tk, _ptr(draft_logits), db, dk, code, n, k, v,
+          _ptr(draft_tokens), _ptr(accept_u), _ptr(sample_u), _ptr(draft_lengths), float(temperature), float(draft_temperature),
+          _ptr(tokens_out), _ptr(n_accepted_out), _ptr(logprobs_out), _ptr(workspace), workspace.numel(), _raw_stream(stream, dev.index))
     return tokens_out, n_accepted_out, logprobs_out
 
 
@@ -805,6 +821,10 @@ def grpo_block_norm_fwd(residual, block=None, post_weight=None, gate=None, pre_w
     """Returns (residual_out, hidden): residual + residual_scale * gate * norm(block) * post_weight, and its norm times
     pre_weight (None without one); see grpo_block_norm_fwd in grpo.h.  ``gate`` is [n_tokens, d_model], or [d_model] for all
     rows.  Without a block residual_out is residual itself; ``inplace=True`` writes over it."""
+    if residual_out is None and hidden is None and not inplace and stream is None:
+        out = _fast.block_norm_fwd(residual, block, post_weight, gate, pre_weight, residual_scale, eps)
+        if out is not None:
+            return _fast_result(out, "grpo_block_norm_fwd")
     dtype = next((t.dtype for t in (block, pre_weight) if t is not None), residual.dtype)
     dev, n, d, rs, fs, gs = _block_norm_args(residual, block, post_weight, gate, pre_weight, dtype)
     os_ = hs = 0
@@ -822,11 +842,9 @@ def grpo_block_norm_fwd(residual, block=None, post_weight=None, gate=None, pre_w
         hs = _block_norm_rows(hidden, "hidden", dtype, n, d, dev)
     elif hidden is not None:
         raise ValueError("hidden is written only where there is a pre_weight")
-    rc = lib().grpo_block_norm_fwd(_ptr(residual), rs, _DTYPE_CODES[residual.dtype], _ptr(block), fs, _ptr(post_weight), _ptr(gate), gs,
-                                   _ptr(pre_weight), _DTYPE_CODES[dtype], n, d, float(residual_scale), float(eps), _ptr(residual_out),
-                                   os_, _ptr(hidden), hs, _raw_stream(stream, dev.index))
-    if rc != GRPO_OK:
-        raise GrpoError(rc, "grpo_block_norm_fwd")
+    _call("grpo_block_norm_fwd", dev, lib().grpo_block_norm_fwd, _ptr(residual), rs, _DTYPE_CODES[residual.dtype], _ptr(block), fs,
+          _ptr(post_weight), _ptr(gate), gs, _ptr(pre_weight), _DTYPE_CODES[dtype], n, d, float(residual_scale), float(eps),
+          _ptr(residual_out), os_, _ptr(hidden), hs, _raw_stream(stream, dev.index))
     return (residual if block is None else residual_out), hidden
 
 
@@ -837,6 +855,11 @@ def grpo_block_norm_bwd(residual_out, block=None, post_weight=None, gate=None, p
 
     Returns (grad_residual, grad_block, grad_gate, grad_post_weight, grad_pre_weight), None for what there is not.  The
     gradients of the weights, and of a gate for all rows, are f32 [d_model]."""
+    if grad_residual is None and grad_block is None and grad_gate is None and grad_post_weight is None and grad_pre_weight is None and \
+            not accumulate_grad_weights and workspace is None and stream is None:
+        out = _fast.block_norm_bwd(residual_out, block, post_weight, gate, pre_weight, grad_hidden, grad_residual_out, residual_scale, eps)
+        if out is not None:
+            return _fast_result(out, "grpo_block_norm_bwd")
     dtype = next((t.dtype for t in (block, pre_weight) if t is not None), residual_out.dtype)
     dev, n, d, rs, fs, gs = _block_norm_args(residual_out, block, post_weight, gate, pre_weight, dtype)
     if (grad_hidden is None) != (pre_weight is None):
@@ -873,13 +896,11 @@ def grpo_block_norm_bwd(residual_out, block=None, post_weight=None, gate=None, p
     L = lib()
     if workspace is None:
         workspace = torch.empty(L.grpo_block_norm_workspace_bytes(n, d), dtype=torch.uint8, device=dev)
-    rc = L.grpo_block_norm_bwd(_ptr(residual_out) if pre_weight is not None else None, rs, _DTYPE_CODES[residual_out.dtype], _ptr(block), fs,
-                               _ptr(post_weight), _ptr(gate), gs, _ptr(pre_weight), _DTYPE_CODES[dtype], n, d, float(residual_scale),
-                               float(eps), _ptr(grad_hidden), hs, _ptr(grad_residual_out), os_, _ptr(grad_residual), dxs, _ptr(grad_block),
-                               dfs, _ptr(grad_gate), dgs, _ptr(grad_post_weight), _ptr(grad_pre_weight),
-                               1 if accumulate_grad_weights else 0, _ptr(workspace), workspace.numel(), _raw_stream(stream, dev.index))
-    if rc != GRPO_OK:
-        raise GrpoError(rc, "grpo_block_norm_bwd")
+    _call("grpo_block_norm_bwd", dev, L.grpo_block_norm_bwd, _ptr(residual_out) if pre_weight is not None else None, rs,
+          _DTYPE_CODES[residual_out.dtype], _ptr(block), fs, _ptr(post_weight), _ptr(gate), gs, _ptr(pre_weight), _DTYPE_CODES[dtype], n, d,
+          float(residual_scale), float(eps), _ptr(grad_hidden), hs, _ptr(grad_residual_out), os_, _ptr(grad_residual), dxs,
+          _ptr(grad_block), dfs, _ptr(grad_gate), dgs, _ptr(grad_post_weight), _ptr(grad_pre_weight), 1 if accumulate_grad_weights else 0,
+          _ptr(workspace), workspace.numel(), _raw_stream(stream, dev.index))
     return grad_residual, grad_block, grad_gate, grad_post_weight, grad_pre_weight
 
 
@@ -889,7 +910,7 @@ class OptimPlan:
 
     def __init__(self, plan, table, tensors):
         self._plan, self._table, self._tensors = plan, table, tensors
-        self._by_ref = ctypes.byref(plan)
+        self._address = ctypes.addressof(plan)
 
     @property
     def device(self):
@@ -964,6 +985,10 @@ def grpo_optim_plan(params, grads, exp_avgs=None, exp_avg_sqs=None, *, masters=N
 def grpo_grad_norm(plan, max_norm=0.0, *, norm_out=None, workspace=None, stream=None):
     """[2] f32: the norm of all the plan's gradients, and the coefficient that clips it at max_norm (1 where there is none);
     see grpo_grad_norm in grpo.h."""
+    if norm_out is None and workspace is None and stream is None:
+        out = _fast.grad_norm(plan._address, plan._table, max_norm)
+        if out is not None:
+            return _fast_result(out, "grpo_grad_norm")
     dev = plan.device
     if norm_out is None:
         norm_out = torch.empty(2, dtype=torch.float32, device=dev)
@@ -972,10 +997,8 @@ def grpo_grad_norm(plan, max_norm=0.0, *, norm_out=None, workspace=None, stream=
     L = lib()
     if workspace is None:
         workspace = torch.empty(L.grpo_grad_norm_workspace_bytes(), dtype=torch.uint8, device=dev)
-    rc = L.grpo_grad_norm(plan._by_ref, _ptr(plan._table), float(max_norm), _ptr(norm_out), _ptr(workspace), workspace.numel(),
-                          _raw_stream(stream, dev.index))
-    if rc != GRPO_OK:
-        raise GrpoError(rc, "grpo_grad_norm")
+    _call("grpo_grad_norm", dev, L.grpo_grad_norm, plan._address, _ptr(plan._table), float(max_norm), _ptr(norm_out), _ptr(workspace),
+          workspace.numel(), _raw_stream(stream, dev.index))
     return norm_out
 
 
@@ -984,6 +1007,11 @@ def grpo_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, *, clip=No
 
     ``step`` counts from 1; ``step`` (i64) and ``lr`` (f32) may be device tensors of one value, which a captured graph reads at
     every replay.  ``clip``: what grpo_grad_norm returned."""
+    if stream is None:
+        out = _fast.adamw_step(plan._address, plan._table, step, lr, beta1, beta2, eps, clip)
+        if out is not None:
+            _fast_result(out, "grpo_adamw_step")
+            return
     dev = plan.device
     step_at = lr_at = None
     if isinstance(step, torch.Tensor):
@@ -994,7 +1022,5 @@ def grpo_adamw_step(plan, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, *, clip=No
         lr, lr_at = 0.0, _ptr(lr)
     if clip is not None:
         _check(clip, torch.float32, 2, "clip", dev)
-    rc = lib().grpo_adamw_step(plan._by_ref, _ptr(plan._table), int(step), step_at, float(lr), lr_at, float(beta1), float(beta2),
-                               float(eps), _ptr(clip), _raw_stream(stream, dev.index))
-    if rc != GRPO_OK:
-        raise GrpoError(rc, "grpo_adamw_step")
+    _call("grpo_adamw_step", dev, lib().grpo_adamw_step, plan._address, _ptr(plan._table), int(step), step_at, float(lr), lr_at,
+          float(beta1), float(beta2), float(eps), _ptr(clip), _raw_stream(stream, dev.index))

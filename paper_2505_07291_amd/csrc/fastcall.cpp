@@ -32,6 +32,15 @@ decltype(&grpo_total_rewards) f_total_rewards;
 decltype(&grpo_filter_groups) f_filter_groups;
 decltype(&grpo_packed_layout) f_packed_layout;
 bool bound = false;
+decltype(&grpo_verify_workspace_bytes) f_verify_workspace_bytes;
+decltype(&grpo_verify_drafts) f_verify_drafts;
+decltype(&grpo_block_norm_workspace_bytes) f_block_norm_workspace_bytes;
+decltype(&grpo_block_norm_fwd) f_block_norm_fwd;
+decltype(&grpo_block_norm_bwd) f_block_norm_bwd;
+decltype(&grpo_grad_norm_workspace_bytes) f_grad_norm_workspace_bytes;
+decltype(&grpo_grad_norm) f_grad_norm;
+decltype(&grpo_adamw_step) f_adamw_step;
+bool operators_bound = false;
 
 // Are all functionalities of `keys` among the usual ones?  (Which backends the keys name is not looked at.)
 bool only(c10::DispatchKeySet keys, c10::DispatchKeySet usual)
@@ -345,6 +354,230 @@ PyObject *loss_aux_fwd_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
     END_HANDLE_TH_ERRORS
 }
 
+// ---- verification of drafted tokens, a block's norms, the gradients' norm, AdamW: calls on the current device ----
+
+bool here(const c10::Device &dev) { return operators_bound && dev.index() == c10::hip::current_device(); }
+bool dtype_of(const at::Tensor *t, grpo_dtype *out)
+{
+    *out = t->scalar_type() == at::kBFloat16 ? GRPO_BF16 : GRPO_F32;
+    return t->scalar_type() == at::kBFloat16 || t->scalar_type() == at::kFloat;
+}
+int64_t whole_vectors(int64_t n, at::ScalarType type)  // entries of rows that begin on 16-byte boundaries
+{
+    const int64_t per16 = type == at::kBFloat16 ? 8 : 4;
+    return (n + per16 - 1) / per16 * per16;
+}
+// an [n, d] tensor of this type whose rows have unit stride, or nullptr; its pitch
+const at::Tensor *rows(PyObject *o, at::ScalarType type, int64_t n, int64_t d, const c10::Device &dev, int64_t *pitch)
+{
+    const at::Tensor *t = plain(o);
+    if (!t || t->scalar_type() != type || t->dim() != 2 || t->size(0) != n || t->size(1) != d || (t->stride(1) != 1 && d > 1) || t->device() != dev)
+        return nullptr;
+    *pitch = n > 1 ? t->stride(0) : std::max<int64_t>(t->stride(0), d);
+    return t;
+}
+at::Tensor new_rows(int64_t n, int64_t d, at::ScalarType type, const c10::Device &dev)
+{
+    const int64_t pitch = whole_vectors(d, type);
+    const at::Tensor t = at::empty({n, pitch}, at::TensorOptions().dtype(type).device(dev));
+    return pitch == d ? t : t.narrow(1, 0, d);
+}
+
+// verify_drafts(target_logits, draft_logits or None, draft_tokens or None, accept_u or None, sample_u, draft_lengths or None,
+//               temperature, draft_temperature)
+PyObject *verify_drafts(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    double temperature, draft_temperature;
+    ORDINARY(n_args == 8 && plain_mode() && number(a[6], &temperature) && number(a[7], &draft_temperature));
+    const at::Tensor *target = plain(a[0]), *draft = nullptr, *tokens = nullptr, *u = nullptr, *lengths;
+    grpo_dtype dtype;
+    ORDINARY(target && target->dim() == 3 && dtype_of(target, &dtype) && target->size(1) > 0);
+    const c10::Device dev = target->device();
+    const int64_t n = target->size(0), k = target->size(1) - 1, v = target->size(2), pitch = whole_vectors(v, target->scalar_type());
+    ORDINARY(here(dev) && n > 0 && v > 0 && (target->stride(2) == 1 || v == 1));
+    const int64_t tb = n > 1 ? target->stride(0) : 0, tk = k > 0 ? target->stride(1) : pitch;
+    int64_t db = 0, dk = 0;
+    if (k > 0) {
+        if (a[1] != Py_None) {
+            draft = plain(a[1]);
+            ORDINARY(draft && draft->dim() == 3 && draft->scalar_type() == target->scalar_type() && draft->device() == dev && draft->size(0) == n &&
+                     draft->size(1) == k && draft->size(2) == v && (draft->stride(2) == 1 || v == 1));
+            db = n > 1 ? draft->stride(0) : 0;
+            dk = k > 1 ? draft->stride(1) : pitch;
+        }
+        tokens = plain(a[2]);
+        u = plain(a[3]);
+        ORDINARY(tokens && tokens->scalar_type() == at::kLong && tokens->dim() == 2 && tokens->size(0) == n && tokens->size(1) == k &&
+                 tokens->is_contiguous() && tokens->device() == dev);
+        ORDINARY(u && u->scalar_type() == at::kFloat && u->dim() == 2 && u->size(0) == n && u->size(1) == k && u->is_contiguous() &&
+                 u->device() == dev);
+    } else {
+        ORDINARY((a[2] == Py_None || plain(a[2])) && (a[3] == Py_None || plain(a[3])));
+    }
+    const at::Tensor *sample = row(a[4], at::kDouble, n, &dev);
+    ORDINARY(sample && row_or_none(a[5], at::kInt, n, &dev, &lengths));
+    const auto of = [&](at::ScalarType type) { return at::TensorOptions().dtype(type).device(dev); };
+    at::Tensor out = at::empty({n, k + 1}, of(at::kLong)), accepted = make(n, at::kInt, dev), lp = at::empty({n, k + 1}, of(at::kFloat)),
+               ws = make((int64_t)f_verify_workspace_bytes(n, k, v, dtype), at::kByte, dev);
+    void *st = current_stream();
+    const grpo_status rc = call(f_verify_drafts, ptr(target), tb, tk, ptr(draft), db, dk, dtype, n, k, v, as<const int64_t>(tokens),
+                                as<const float>(u), as<const double>(sample), as<const int32_t>(lengths), temperature, draft_temperature,
+                                as<int64_t>(out), as<int32_t>(accepted), as<float>(lp), ptr(ws), (size_t)ws.numel(), st);
+    return rc == GRPO_OK ? tuple_of({out, accepted, lp}) : PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+struct NormArgs {
+    const at::Tensor *residual, *block = nullptr, *post, *gate = nullptr, *pre;
+    c10::Device dev = c10::Device(c10::kCPU);
+    at::ScalarType type;
+    grpo_dtype residual_dtype, dtype;
+    int64_t n, d, rs, fs = 0, gs = 0;
+    double scale, eps;
+};
+// residual, block, post_weight, gate, pre_weight in a[0] .. a[4], scale and eps in a[at] and a[at + 1]
+bool norm_args(PyObject *const *a, int at, NormArgs *p)
+{
+    p->residual = plain(a[0]);
+    if (!p->residual || p->residual->dim() != 2 || !dtype_of(p->residual, &p->residual_dtype) || !number(a[at], &p->scale) ||
+        !number(a[at + 1], &p->eps))
+        return false;
+    p->dev = p->residual->device();
+    p->n = p->residual->size(0);
+    p->d = p->residual->size(1);
+    if (!here(p->dev) || p->n == 0 || p->d == 0 || !rows(a[0], p->residual->scalar_type(), p->n, p->d, p->dev, &p->rs)) return false;
+    const at::Tensor *of = plain(a[1] != Py_None ? a[1] : a[4]);
+    if (!of || !dtype_of(of, &p->dtype)) return false;
+    p->type = of->scalar_type();
+    if (a[1] != Py_None && !(p->block = rows(a[1], p->type, p->n, p->d, p->dev, &p->fs))) return false;
+    if (!row_or_none(a[2], p->type, p->d, &p->dev, &p->post) || !row_or_none(a[4], p->type, p->d, &p->dev, &p->pre)) return false;
+    if (a[3] == Py_None) return true;
+    p->gate = plain(a[3]);
+    if (!p->gate) return false;
+    if (p->gate->dim() == 1) return row(a[3], p->type, p->d, &p->dev) != nullptr;
+    return rows(a[3], p->type, p->n, p->d, p->dev, &p->gs) != nullptr && p->gs != 0;
+}
+
+// block_norm_fwd(residual, block or None, post_weight or None, gate or None, pre_weight or None, residual_scale, eps)
+PyObject *block_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    NormArgs p;
+    ORDINARY(n_args == 7 && plain_mode() && norm_args(a, 5, &p));
+    at::Tensor out, hidden;
+    if (p.block) out = new_rows(p.n, p.d, p.residual->scalar_type(), p.dev);
+    if (p.pre) hidden = new_rows(p.n, p.d, p.type, p.dev);
+    void *st = current_stream();
+    const grpo_status rc = call(f_block_norm_fwd, ptr(p.residual), p.rs, p.residual_dtype, ptr(p.block), p.fs, ptr(p.post), ptr(p.gate), p.gs,
+                                ptr(p.pre), p.dtype, p.n, p.d, p.scale, p.eps, p.block ? ptr(out) : nullptr, p.block ? out.stride(0) : 0,
+                                p.pre ? ptr(hidden) : nullptr, p.pre ? hidden.stride(0) : 0, st);
+    return rc == GRPO_OK ? tuple_of({p.block ? out : *p.residual, hidden}) : PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// block_norm_bwd(residual_out, block or None, post_weight or None, gate or None, pre_weight or None, grad_hidden or None,
+//                grad_residual_out or None, residual_scale, eps)
+PyObject *block_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    NormArgs p;
+    ORDINARY(n_args == 9 && plain_mode() && norm_args(a, 7, &p) && (a[5] == Py_None) == (p.pre == nullptr));
+    const at::ScalarType rt = p.residual->scalar_type();
+    const at::Tensor *dh = nullptr, *dxo = nullptr;
+    int64_t dhs = 0, dxos = 0;
+    ORDINARY(a[5] == Py_None || (dh = rows(a[5], p.type, p.n, p.d, p.dev, &dhs)));
+    ORDINARY(a[6] == Py_None || (dxo = rows(a[6], rt, p.n, p.d, p.dev, &dxos)));
+    at::Tensor dx = new_rows(p.n, p.d, rt, p.dev), df, dg, dw1, dw2, ws = make((int64_t)f_block_norm_workspace_bytes(p.n, p.d), at::kByte, p.dev);
+    if (p.block) df = new_rows(p.n, p.d, p.type, p.dev);
+    if (p.gate) dg = p.gs ? new_rows(p.n, p.d, p.type, p.dev) : make(p.d, at::kFloat, p.dev);
+    if (p.post) dw1 = make(p.d, at::kFloat, p.dev);
+    if (p.pre) dw2 = make(p.d, at::kFloat, p.dev);
+    const auto at_ = [](const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+    void *st = current_stream();
+    const grpo_status rc = call(f_block_norm_bwd, p.pre ? ptr(p.residual) : nullptr, p.rs, p.residual_dtype, ptr(p.block), p.fs, ptr(p.post),
+                                ptr(p.gate), p.gs, ptr(p.pre), p.dtype, p.n, p.d, p.scale, p.eps, ptr(dh), dhs, ptr(dxo), dxos, ptr(dx),
+                                dx.stride(0), at_(df), p.block ? df.stride(0) : 0, at_(dg), p.gs ? dg.stride(0) : 0, (float *)at_(dw1),
+                                (float *)at_(dw2), 0, ptr(ws), (size_t)ws.numel(), st);
+    return rc == GRPO_OK ? tuple_of({dx, df, dg, dw1, dw2}) : PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// The address of an OptimPlan's grpo_optim_plan, and its table.
+bool plan_of(PyObject *address, PyObject *table, const grpo_optim_plan **plan, const at::Tensor **t)
+{
+    if (!PyLong_CheckExact(address)) return false;
+    *plan = (const grpo_optim_plan *)PyLong_AsVoidPtr(address);
+    if (!*plan) {
+        PyErr_Clear();
+        return false;
+    }
+    *t = row(table, at::kByte, -1, nullptr);
+    return *t && here((*t)->device());
+}
+
+// grad_norm(plan's address, table, max_norm)
+PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    double most;
+    const grpo_optim_plan *plan;
+    const at::Tensor *table;
+    ORDINARY(n_args == 3 && plain_mode() && number(a[2], &most) && plan_of(a[0], a[1], &plan, &table));
+    const c10::Device dev = table->device();
+    at::Tensor out = make(2, at::kFloat, dev), ws = make((int64_t)f_grad_norm_workspace_bytes(), at::kByte, dev);
+    void *st = current_stream();
+    const grpo_status rc = call(f_grad_norm, plan, ptr(table), most, as<float>(out), ptr(ws), (size_t)ws.numel(), st);
+    return rc == GRPO_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
+    END_HANDLE_TH_ERRORS
+}
+
+// adamw_step(plan's address, table, step, lr, beta1, beta2, eps, clip or None): True
+PyObject *adamw_step(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    HANDLE_TH_ERRORS
+    int64_t step;
+    double f[4];
+    const grpo_optim_plan *plan;
+    const at::Tensor *table, *clip;
+    ORDINARY(n_args == 8 && plain_mode() && whole(a[2], &step) && plan_of(a[0], a[1], &plan, &table));
+    for (int i = 0; i < 4; ++i) ORDINARY(number(a[3 + i], &f[i]));
+    const c10::Device dev = table->device();
+    ORDINARY(row_or_none(a[7], at::kFloat, 2, &dev, &clip));
+    void *st = current_stream();
+    const grpo_status rc = call(f_adamw_step, plan, ptr(table), step, nullptr, f[0], nullptr, f[1], f[2], f[3], as<const float>(clip), st);
+    if (rc != GRPO_OK) return PyLong_FromLong(rc);
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
+// bind_operators(addresses in the order below): those of the functions behind the line above
+PyObject *bind_operators(PyObject *, PyObject *const *a, Py_ssize_t n_args)
+{
+    void *at[8];
+    if (n_args != 8) {
+        PyErr_SetString(PyExc_TypeError, "bind_operators takes eight addresses");
+        return nullptr;
+    }
+    for (int i = 0; i < 8; ++i) {
+        at[i] = PyLong_AsVoidPtr(a[i]);
+        if (!at[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a function's address is not null");
+            return nullptr;
+        }
+    }
+    f_verify_workspace_bytes = (decltype(f_verify_workspace_bytes))at[0];
+    f_verify_drafts = (decltype(f_verify_drafts))at[1];
+    f_block_norm_workspace_bytes = (decltype(f_block_norm_workspace_bytes))at[2];
+    f_block_norm_fwd = (decltype(f_block_norm_fwd))at[3];
+    f_block_norm_bwd = (decltype(f_block_norm_bwd))at[4];
+    f_grad_norm_workspace_bytes = (decltype(f_grad_norm_workspace_bytes))at[5];
+    f_grad_norm = (decltype(f_grad_norm))at[6];
+    f_adamw_step = (decltype(f_adamw_step))at[7];
+    operators_bound = true;
+    Py_RETURN_NONE;
+}
+
 // bind(addresses in the order below): the library that calls go to from now on
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 {
@@ -375,6 +608,8 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n_args)
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind),           METHOD(total_rewards), METHOD(filter_groups), METHOD(packed_layout),
                          METHOD(group_advantages), METHOD(logprobs_fwd),  METHOD(loss_fwd_bwd),  METHOD(loss_aux_fwd_bwd),
+                         METHOD(bind_operators), METHOD(verify_drafts), METHOD(block_norm_fwd), METHOD(block_norm_bwd),
+                         METHOD(grad_norm),      METHOD(adamw_step),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
