@@ -6,8 +6,8 @@
 //   m  = beta1 m + (1 - beta1) g'          v = beta2 v + (1 - beta2) g'^2
 //   p  = p (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
 //
-// Both walk over a table in device memory, made once by grpo_optim_plan_build: the tensors, and for every 8192 values of
-// them which tensor and which 8192 (a look-up by a value's index would be ten dependent loads with a thousand tensors).  So a
+// Both walk over a table in device memory, made once by grpo_optim_plan_build: the tensors, and for every 4096 values of
+// them which tensor and which 4096 (a look-up by a value's index would be ten dependent loads with a thousand tensors).  So a
 // model of any number of tensors is one launch, whose workgroups all have the same work.
 //
 // Values are taken 256 at a time by a wavefront, which are also the 256 that share a scale of the 8-bit moments: four
@@ -33,7 +33,7 @@ struct OptChunk {
 
 constexpr int kOptBlock = 256;
 constexpr int kOptQuant = 256;    // values to a scale, and to a wavefront's step
-constexpr int kOptChunk = 8192;   // values to a workgroup of adamw_step_k
+constexpr int kOptChunk = 4096;   // values to a workgroup of adamw_step_k
 constexpr long long kOptMaxValues = 1ll << 40;  // of one tensor
 constexpr int kNormBlocks = 2048; // workgroups, and partial sums, of grad_norm_k
 
@@ -170,66 +170,85 @@ struct AdamWStep {  // the same for a whole workgroup
     float coef, decay, step_size, inv_root;
 };
 
-// 256 values of a tensor from value `at` on, of which `left` are there.
-template <int PARAM, bool GBF16, bool STATE8, bool WIDE>
-__device__ __forceinline__ void adamw_256(const AdamW &a, const AdamWStep &s, const OptTensor &t, long long at, int left, int lane)
+// U times 256 values of a tensor, from value `at` on and every `step`; of the last 256 `left` are there.  Everything is asked for
+// before anything is written: the compiler cannot move a load in front of a store.
+template <int PARAM, bool GBF16, bool STATE8, bool WIDE, int U>
+__device__ __forceinline__ void adamw_256(const AdamW &a, const AdamWStep &s, const OptTensor &t, long long at, int step, int left, int lane)
 {
-    float g[4], m[4], v[4], p[4];
-    if constexpr (GBF16)
-        load4_bf16<WIDE>((const unsigned short *)t.grad + at, lane, left, g);
-    else
-        load4_f32<WIDE>((const float *)t.grad + at, lane, left, g);
-    const long long block = at / kOptQuant;
-    if constexpr (STATE8) {
-        load4_e4m3<WIDE>((const unsigned char *)t.m + at, lane, left, t.m_scale[block], m);
-        load4_e4m3<WIDE>((const unsigned char *)t.v + at, lane, left, t.v_scale[block], v);
-    } else {
-        load4_f32<WIDE>((const float *)t.m + at, lane, left, m);
-        load4_f32<WIDE>((const float *)t.v + at, lane, left, v);
-    }
-    if constexpr (PARAM == kParamF32)
-        load4_f32<WIDE>((const float *)t.param + at, lane, left, p);
-    else if constexpr (PARAM == kParamBf16)
-        load4_bf16<WIDE>((const unsigned short *)t.param + at, lane, left, p);
-    else
-        load4_f32<WIDE>(t.master + at, lane, left, p);
-    float r[4];
+    float g[U][4], m[U][4], v[U][4], p[U][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        // Every operation is rounded by itself, in this order: what a step gives does not hang on which sums the compiler
-        // fuses, and 8-bit moments are rounded from values that anybody can compute again.
-#pragma clang fp contract(off)
-        const float gc = g[j] * s.coef;
-        if constexpr (STATE8) v[j] = v[j] * v[j];  // sqrt(v) is what is held
-        m[j] = m[j] * a.beta1 + gc * a.one_beta1;
-        v[j] = v[j] * a.beta2 + gc * gc * a.one_beta2;
-        r[j] = __builtin_sqrtf(v[j]);
-        const float step = m[j] / (r[j] * s.inv_root + a.eps);
-        p[j] = p[j] * s.decay - step * s.step_size;
+    for (int u = 0; u < U; ++u) {
+        const long long i = at + u * step, block = i / kOptQuant;
+        if constexpr (GBF16)
+            load4_bf16<WIDE>((const unsigned short *)t.grad + i, lane, left, g[u]);
+        else
+            load4_f32<WIDE>((const float *)t.grad + i, lane, left, g[u]);
+        if constexpr (STATE8) {
+            load4_e4m3<WIDE>((const unsigned char *)t.m + i, lane, left, t.m_scale[block], m[u]);
+            load4_e4m3<WIDE>((const unsigned char *)t.v + i, lane, left, t.v_scale[block], v[u]);
+        } else {
+            load4_f32<WIDE>((const float *)t.m + i, lane, left, m[u]);
+            load4_f32<WIDE>((const float *)t.v + i, lane, left, v[u]);
+        }
+        if constexpr (PARAM == kParamF32)
+            load4_f32<WIDE>((const float *)t.param + i, lane, left, p[u]);
+        else if constexpr (PARAM == kParamBf16)
+            load4_bf16<WIDE>((const unsigned short *)t.param + i, lane, left, p[u]);
+        else
+            load4_f32<WIDE>(t.master + i, lane, left, p[u]);
     }
-    if constexpr (PARAM != kParamF32) store4_bf16<WIDE>((unsigned short *)t.param + at, lane, left, p);
-    if constexpr (PARAM == kParamF32) store4_f32<WIDE>((float *)t.param + at, lane, left, p);
-    if constexpr (PARAM == kParamMaster) store4_f32<WIDE>(t.master + at, lane, left, p);
-    if constexpr (STATE8) {
-        store4_e4m3<WIDE, false>((unsigned char *)t.m + at, t.m_scale + block, lane, left, m);
-        store4_e4m3<WIDE, true>((unsigned char *)t.v + at, t.v_scale + block, lane, left, r);
-    } else {
-        store4_f32<WIDE>((float *)t.m + at, lane, left, m);
-        store4_f32<WIDE>((float *)t.v + at, lane, left, v);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const long long i = at + u * step, block = i / kOptQuant;
+        float r[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            // Every operation is rounded by itself, in this order: what a step gives does not hang on which sums the compiler
+            // fuses, and 8-bit moments are rounded from values that anybody can compute again.
+#pragma clang fp contract(off)
+            const float gc = g[u][j] * s.coef;
+            if constexpr (STATE8) v[u][j] = v[u][j] * v[u][j];  // sqrt(v) is what is held
+            m[u][j] = m[u][j] * a.beta1 + gc * a.one_beta1;
+            v[u][j] = v[u][j] * a.beta2 + gc * gc * a.one_beta2;
+            r[j] = __builtin_sqrtf(v[u][j]);
+            const float move = m[u][j] / (r[j] * s.inv_root + a.eps);
+            p[u][j] = p[u][j] * s.decay - move * s.step_size;
+        }
+        if constexpr (PARAM != kParamF32) store4_bf16<WIDE>((unsigned short *)t.param + i, lane, left, p[u]);
+        if constexpr (PARAM == kParamF32) store4_f32<WIDE>((float *)t.param + i, lane, left, p[u]);
+        if constexpr (PARAM == kParamMaster) store4_f32<WIDE>(t.master + i, lane, left, p[u]);
+        if constexpr (STATE8) {
+            store4_e4m3<WIDE, false>((unsigned char *)t.m + i, t.m_scale + block, lane, left, m[u]);
+            store4_e4m3<WIDE, true>((unsigned char *)t.v + i, t.v_scale + block, lane, left, r);
+        } else {
+            store4_f32<WIDE>((float *)t.m + i, lane, left, m[u]);
+            store4_f32<WIDE>((float *)t.v + i, lane, left, v[u]);
+        }
     }
 }
 
+// 256s that a wavefront asks for at a time.  123 million values with 8-bit moments take 345 us by four, 364 by two and 374 one by one, and
+// 338 where those four are all a workgroup does (kOptChunk; at 16384 370); 778 million with fp32 moments and a master copy
+// 4.32 ms and 4.18 (5.6 TB/s).  Loads or stores that may stay in the caches cost 3 to 9 %.
+constexpr int kOptAhead = 4;
 template <int PARAM, bool GBF16, bool STATE8>
 __device__ __forceinline__ void adamw_chunk(const AdamW &a, const AdamWStep &s, const OptTensor &t, long long first)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int kStep = kOptBlock / 64 * kOptQuant;
+    if (t.wide && t.n - first >= kOptChunk) {
+#pragma unroll 1
+        for (int i = 0; i < kOptChunk; i += kOptAhead * kStep)
+            adamw_256<PARAM, GBF16, STATE8, true, kOptAhead>(a, s, t, first + i + wave * kOptQuant, kStep, kOptQuant, lane);
+        return;
+    }
     const long long end = t.n - first < kOptChunk ? t.n : first + kOptChunk;
-    for (long long at = first + wave * kOptQuant; at < end; at += kOptBlock / 64 * kOptQuant) {
+    for (long long at = first + wave * kOptQuant; at < end; at += kStep) {
         const int left = end - at < kOptQuant ? (int)(end - at) : kOptQuant;
         if (t.wide && left == kOptQuant)
-            adamw_256<PARAM, GBF16, STATE8, true>(a, s, t, at, left, lane);
+            adamw_256<PARAM, GBF16, STATE8, true, 1>(a, s, t, at, 0, left, lane);
         else
-            adamw_256<PARAM, GBF16, STATE8, false>(a, s, t, at, left, lane);
+            adamw_256<PARAM, GBF16, STATE8, false, 1>(a, s, t, at, 0, left, lane);
     }
 }
 
@@ -272,41 +291,53 @@ static __global__ void __launch_bounds__(kOptBlock) adamw_step_k(AdamW a)
 
 // Squares are exact in fp64 and summed there, each workgroup's chunks in the table's order and the workgroups' sums in theirs:
 // the same gradients always give the same norm.
+template <bool GBF16, bool WIDE>
+__device__ __forceinline__ void load4_grad(const OptTensor &t, long long at, int lane, int left, float (&g)[4])
+{
+    if constexpr (GBF16)
+        load4_bf16<WIDE>((const unsigned short *)t.grad + at, lane, left, g);
+    else
+        load4_f32<WIDE>((const float *)t.grad + at, lane, left, g);
+}
 template <bool GBF16>
 __device__ __forceinline__ double norm_chunk(const OptTensor &t, long long first)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long end = t.n - first < kOptChunk ? t.n : first + kOptChunk;
+    constexpr int kStep = kOptBlock / 64 * kOptQuant, U = kOptChunk / kStep;
     double sum = 0.0;
-    for (long long at = first + wave * kOptQuant; at < end; at += kOptBlock / 64 * kOptQuant) {
+    if (t.wide && t.n - first >= kOptChunk) {
+        float g[U][4];
+#pragma unroll
+        for (int u = 0; u < U; ++u) load4_grad<GBF16, true>(t, first + u * kStep + wave * kOptQuant, lane, kOptQuant, g[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum += (double)g[u][j] * (double)g[u][j];
+        return sum;
+    }
+    const long long end = t.n - first < kOptChunk ? t.n : first + kOptChunk;
+    for (long long at = first + wave * kOptQuant; at < end; at += kStep) {
         const int left = end - at < kOptQuant ? (int)(end - at) : kOptQuant;
         float g[4];
-        const bool wide = t.wide && left == kOptQuant;
-        if constexpr (GBF16) {
-            if (wide)
-                load4_bf16<true>((const unsigned short *)t.grad + at, lane, left, g);
-            else
-                load4_bf16<false>((const unsigned short *)t.grad + at, lane, left, g);
-        } else {
-            if (wide)
-                load4_f32<true>((const float *)t.grad + at, lane, left, g);
-            else
-                load4_f32<false>((const float *)t.grad + at, lane, left, g);
-        }
+        if (t.wide && left == kOptQuant)
+            load4_grad<GBF16, true>(t, at, lane, left, g);
+        else
+            load4_grad<GBF16, false>(t, at, lane, left, g);
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum += (double)g[j] * (double)g[j];
     }
     return sum;
 }
 
-__device__ __forceinline__ double block_sum_f64(double v, double *lds)  // of kOptBlock lanes, to all of them
+template <int BLOCK>
+__device__ __forceinline__ double block_sum_f64(double v, double *lds)  // to all lanes
 {
     v = wave_sum_dpp(v);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < kOptBlock / 64; ++i) s += lds[i];
+    for (int i = 0; i < BLOCK / 64; ++i) s += lds[i];
     return s;
 }
 
@@ -320,16 +351,17 @@ static __global__ void __launch_bounds__(kOptBlock) grad_norm_k(const OptTensor 
         const long long first = (long long)c.chunk * kOptChunk;
         sum += t.grad_bf16 ? norm_chunk<true>(t, first) : norm_chunk<false>(t, first);
     }
-    sum = block_sum_f64(sum, lds);
+    sum = block_sum_f64<kOptBlock>(sum, lds);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
 }
 
-static __global__ void __launch_bounds__(kOptBlock) grad_norm_total(const double *partial, int n, double max_norm, float *out)
+static __global__ void __launch_bounds__(kNormBlocks / 2) grad_norm_total(const double *partial, int n, double max_norm, float *out)
 {
-    __shared__ double lds[kOptBlock / 64];
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < n; i += kOptBlock) sum += partial[i];
-    const double norm = sqrt(block_sum_f64(sum, lds));
+    constexpr int BLOCK = kNormBlocks / 2;
+    __shared__ double lds[BLOCK / 64];
+    const int i = threadIdx.x;
+    const double a = i < n ? partial[i] : 0.0, b = i + BLOCK < n ? partial[i + BLOCK] : 0.0;
+    const double norm = sqrt(block_sum_f64<BLOCK>(a + b, lds));
     if (threadIdx.x == 0) {
         out[0] = (float)norm;
         out[1] = (float)(!(max_norm > 0.0) || norm <= max_norm ? 1.0 : max_norm / norm);
@@ -456,13 +488,15 @@ grpo_status grpo_grad_norm(const grpo_optim_plan *plan, const void *table, doubl
     if (std::isnan(max_norm)) return GRPO_ERR_PARAM;
     if (!norm_out) return GRPO_ERR_NULL;
     if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < grpo_grad_norm_workspace_bytes()) return GRPO_ERR_WORKSPACE;
-    const int blocks = (int)(plan->n_chunks < kNormBlocks ? plan->n_chunks : kNormBlocks);
+    // as many chunks to each workgroup
+    const int64_t each = (plan->n_chunks + kNormBlocks - 1) / kNormBlocks;
+    const int blocks = each > 0 ? (int)((plan->n_chunks + each - 1) / each) : 0;
     const OptTensor *tensors = (const OptTensor *)table;
     const OptChunk *chunks = (const OptChunk *)((const char *)table + opt_chunks_at(plan->n_tensors));
     if (blocks > 0)
         hipLaunchKernelGGL(grad_norm_k, dim3((unsigned)blocks), dim3(kOptBlock), 0, (hipStream_t)stream, tensors, chunks,
                            (long long)plan->n_chunks, (double *)workspace);
-    hipLaunchKernelGGL(grad_norm_total, dim3(1), dim3(kOptBlock), 0, (hipStream_t)stream, (const double *)workspace, blocks, max_norm, norm_out);
+    hipLaunchKernelGGL(grad_norm_total, dim3(1), dim3(kNormBlocks / 2), 0, (hipStream_t)stream, (const double *)workspace, blocks, max_norm, norm_out);
     return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
 }
 

@@ -155,7 +155,7 @@ def test_plan_sizes_and_refused_buffers():
     sizes = [1, 8192, 8193, 0, 16384]
     tensors = [tensor(P + (i << 24), n) for i, n in enumerate(sizes)]
     rc, plan, need = build(tensors)
-    assert rc == OK and plan.n_tensors == 5 and plan.n_chunks == sum(-(-n // 8192) for n in sizes) and plan.has_params == 1
+    assert rc == OK and plan.n_tensors == 5 and plan.n_chunks == sum(-(-n // 4096) for n in sizes) and plan.has_params == 1
     assert need % 256 == 0 and need >= 5 * 88 + 8 * plan.n_chunks
     assert build(tensors, spare=-1)[0] == WORKSPACE
     assert build(tensors, table=False)[0] == NULL and build(tensors, out=False)[0] == NULL
