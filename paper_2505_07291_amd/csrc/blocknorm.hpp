@@ -11,6 +11,12 @@
 //   df  = r1 (t - y1 mean(t (.) y1))                    dg  = s w1 (.) D (.) y1 (summed over rows where one gate serves all)
 //
 // Both norms' 1/sqrt are formed again in the backward: their sums go along with those it needs anyway.
+//
+// Bound by memory.  Rows stay in registers between the passes over them, so that they are read once: 16384 x 5120 with a residual in fp32,
+// the rest in bf16 and a gate for every row take 190 us forward (14 bytes a value, 6.2 TB/s) and 345 backward (22 bytes,
+// 5.3 TB/s), where kernels that read a row again for every pass took 322 and 1028.  The backward holds 12 registers for each of a
+// lane's values, which leaves two wavefronts to a SIMD: with sums over rows in LDS instead (10 registers) it was no faster
+// (394 us), with the next row asked for in front of the last pass neither (360).
 
 namespace __attribute__((visibility("hidden"))) grpo_impl {
 
@@ -84,7 +90,8 @@ __device__ __forceinline__ void row_store(char *row, int col, int d, const float
     }
 }
 
-constexpr int kNormBlock = 256;
+constexpr int kNormBlock = 256, kWideBlock = 1024;
+constexpr int kWideSums = 19456;  // columns whose two sums fit the LDS of a CU, beside the reductions
 constexpr long long kNormFwdGrid = 65536;
 constexpr long long kNormGrid = 1024;  // workgroups of the backward at most, each with a row of partial sums
 
@@ -101,6 +108,8 @@ __device__ __forceinline__ float row_sum_of(float v, float *lds)
 
 // Where a lane loads from: at column 0 if the row has none for it, and blank() takes out what would go into a sum.  Nothing is under
 // a condition but the stores: what is loaded under one is waited for where it ends, weights of every vector one after the other.
+// (Where rows end inside a vector its loads are.  To patch that vector in behind loads without conditions takes longer: 8192 x
+// 5121 bf16 forward 125 us and 139, backward with an fp32 residual 275 and 335.)
 template <bool RAGGED>
 __device__ __forceinline__ int held_column(int col, int d)
 {
@@ -164,7 +173,7 @@ __global__ void __launch_bounds__(TPR < kNormBlock ? kNormBlock : TPR) block_nor
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const bool there = (i * TPR + t) * VEC < p.d;
-            const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
+            const int col = (i * TPR + t) * VEC;
             xr[i].get(v[i]);
             if (f) {
                 float b[VEC], w[VEC];
@@ -191,7 +200,7 @@ __global__ void __launch_bounds__(TPR < kNormBlock ? kNormBlock : TPR) block_nor
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const bool there = (i * TPR + t) * VEC < p.d;
-            const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
+            const int col = (i * TPR + t) * VEC;
             float w[VEC];
             w2r[i].get(w);
 #pragma unroll
@@ -322,7 +331,6 @@ __global__ void __launch_bounds__(TPR < kNormBlock ? kNormBlock : TPR, 2) block_
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const bool there = (i * TPR + t) * VEC < p.d;
-            const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
             float u[VEC], v[VEC], w[VEC];
             if (p.w2) {
                 blank(xr[i], there);
@@ -351,7 +359,7 @@ __global__ void __launch_bounds__(TPR < kNormBlock ? kNormBlock : TPR, 2) block_
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const bool there = (i * TPR + t) * VEC < p.d;
-            const int col = held_column<RAGGED>((i * TPR + t) * VEC, p.d);
+            const int col = (i * TPR + t) * VEC;
             float u[VEC], v[VEC], w[VEC];
             if (p.dxo) {
                 dr[i].get(D[i]);
@@ -457,17 +465,21 @@ __global__ void __launch_bounds__(TPR < kNormBlock ? kNormBlock : TPR, 2) block_
     }
 }
 
-template <grpo_dtype RT, grpo_dtype DT>
-__global__ void __launch_bounds__(kNormBlock) block_norm_bwd_streamed(BlockNorm p)
+// Wider rows: read again for every pass, each lane's columns the same in all.  The sums over rows are in LDS where they fit (SUMS_LDS),
+// else in the workspace: 4096 x 16384 bf16 358 us
+// and 794, with an fp32 residual 479 and 836.
+template <grpo_dtype RT, grpo_dtype DT, bool SUMS_LDS>
+__global__ void __launch_bounds__(kWideBlock) block_norm_bwd_streamed(BlockNorm p)
 {
+    extern __shared__ __align__(16) float wide_sums[];
     constexpr int VEC = 16 / Elem<RT>::BYTES;
-    __shared__ float lds[4][kNormBlock / 64];
-    float *part = p.part + (size_t)blockIdx.x * 2 * p.d;
+    __shared__ float lds[4][kWideBlock / 64];
+    float *part = p.part + (size_t)blockIdx.x * 2 * p.d, *sums = SUMS_LDS ? wide_sums : part;
     for (long long row = blockIdx.x; row < p.n; row += gridDim.x) {
         const char *x = p.x + row * p.xs, *f = p.f ? p.f + row * p.fs : nullptr, *g = p.g ? p.g + row * p.gs : nullptr;
         const char *dh = p.w2 ? p.dh + row * p.dhs : nullptr, *dxo = p.dxo ? p.dxo + row * p.dxos : nullptr;
         float sx = 0.f, sax = 0.f, sf = 0.f;
-        for (int col = threadIdx.x * VEC; col < p.d; col += kNormBlock * VEC) {
+        for (int col = threadIdx.x * VEC; col < p.d; col += kWideBlock * VEC) {
             float v[VEC], w[VEC], u[VEC];
             if (p.w2) {
                 row_load<RT, VEC>(x, col, p.d, v);
@@ -485,13 +497,13 @@ __global__ void __launch_bounds__(kNormBlock) block_norm_bwd_streamed(BlockNorm 
                 for (int i = 0; i < VEC; ++i) sf += v[i] * v[i];
             }
         }
-        block_sum2<kNormBlock>(sx, sax, lds[0], lds[1]);
-        const float r1 = p.w1 ? 1.f / sqrtf(block_sum<kNormBlock>(sf, lds[2]) * p.inv_d + p.eps) : 1.f;
+        block_sum2<kWideBlock>(sx, sax, lds[0], lds[1]);
+        const float r1 = p.w1 ? 1.f / sqrtf(block_sum<kWideBlock>(sf, lds[2]) * p.inv_d + p.eps) : 1.f;
         const float r2 = 1.f / sqrtf(sx * p.inv_d + p.eps);
         const float c2 = sax * r2 * p.inv_d;  // mean(a y2)
         float sty = 0.f, c1 = 0.f;
         for (int pass = p.w1 ? 0 : 1; pass < 2; ++pass) {
-            for (int col = threadIdx.x * VEC; col < p.d; col += kNormBlock * VEC) {
+            for (int col = threadIdx.x * VEC; col < p.d; col += kWideBlock * VEC) {
                 float v[VEC], w[VEC], u[VEC], D[VEC] = {};
                 if (dxo) row_load<RT, VEC>(dxo, col, p.d, D);
                 if (p.w2) {
@@ -507,7 +519,7 @@ __global__ void __launch_bounds__(kNormBlock) block_norm_bwd_streamed(BlockNorm 
                     if (pass == 1)
 #pragma unroll
                         for (int i = 0; i < VEC; ++i)
-                            if (col + i < p.d) part[col + i] = (row == blockIdx.x ? 0.f : part[col + i]) + v[i];
+                            if (col + i < p.d) sums[col + i] = (row == blockIdx.x ? 0.f : sums[col + i]) + v[i];
                 }
                 if (pass == 1) row_store<RT, VEC>(p.dx + row * p.dxs, col, p.d, D);
                 if (!f) continue;
@@ -535,12 +547,14 @@ __global__ void __launch_bounds__(kNormBlock) block_norm_bwd_streamed(BlockNorm 
                 if (p.dg) row_store<DT, VEC>(p.dg + row * p.dgs, col, p.d, gate);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i)
-                    if (col + i < p.d) part[p.d + col + i] = (row == blockIdx.x ? 0.f : part[p.d + col + i]) + sum[i];
+                    if (col + i < p.d) sums[p.d + col + i] = (row == blockIdx.x ? 0.f : sums[p.d + col + i]) + sum[i];
             }
-            if (pass == 0) c1 = block_sum<kNormBlock>(sty, lds[3]) * p.inv_d;
+            if (pass == 0) c1 = block_sum<kWideBlock>(sty, lds[3]) * p.inv_d;
         }
         __syncthreads();
     }
+    if constexpr (SUMS_LDS)
+        for (int i = threadIdx.x; i < 2 * p.d; i += kWideBlock) part[i] = wide_sums[i];
 }
 
 // The workgroups' sums, added up in fp64: 64 columns to a workgroup, a sixteenth of the sums to each of its wavefronts, which
@@ -627,7 +641,9 @@ static BlockNorm block_norm_params(int rt, int dt, const void *x, int64_t xs, co
 }
 
 // Which kernel takes rows of d: X(lanes to a row, vectors to a lane) of the list for 8 or 4 values to a vector, the first
-// that holds a row, else the streamed one.
+// that holds a row, else the streamed one.  A wavefront to a row, several to a workgroup, as far as its registers go; then as many wavefronts as
+// leave a lane 20 values backward, 32 forward: with fewer the workgroups of a CU are too few to hide what a row waits for (backward of 5120
+// on 640 lanes 399 us, on 320 376, on 256 345), with more its registers run out.
 #define GRPO_NORM_FWD_8(X) X(64, 1) X(64, 2) X(256, 1) X(256, 2) X(320, 2) X(256, 4) X(512, 4)
 #define GRPO_NORM_FWD_4(X) X(64, 1) X(64, 2) X(64, 4) X(256, 2) X(256, 4) X(256, 5) X(256, 8) X(512, 8)
 #define GRPO_NORM_BWD_8(X) X(64, 1) X(64, 2) X(256, 1) X(256, 2) X(320, 2) X(512, 2)
@@ -668,8 +684,20 @@ static int launch_block_norm_bwd_rows(const BlockNorm &p, hipStream_t st)  // wo
         GRPO_NORM_BWD_4(GRPO_NORM_BWD)
     }
 #undef GRPO_NORM_BWD
-    const long long grid = p.n < kNormGrid ? p.n : kNormGrid;
-    hipLaunchKernelGGL((block_norm_bwd_streamed<RT, DT>), dim3((unsigned)grid), dim3(kNormBlock), 0, st, p);
+    const long long cus = cu_count(), grid = p.n < cus ? p.n : cus;
+    if (p.d <= kWideSums) {
+        const unsigned lds = 2u * (unsigned)p.d * 4u;
+        static std::atomic<bool> attr_done[64];  // setting the attribute twice is harmless
+        int dev = 0;
+        if (hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < 64 && !attr_done[dev].load()) {
+            if (hipFuncSetAttribute((const void *)block_norm_bwd_streamed<RT, DT, true>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                    kWideSums * 8) == hipSuccess)
+                attr_done[dev].store(true);
+        }
+        hipLaunchKernelGGL((block_norm_bwd_streamed<RT, DT, true>), dim3((unsigned)grid), dim3(kWideBlock), lds, st, p);
+    } else {
+        hipLaunchKernelGGL((block_norm_bwd_streamed<RT, DT, false>), dim3((unsigned)grid), dim3(kWideBlock), 0, st, p);
+    }
     return (int)grid;
 }
 

@@ -116,8 +116,9 @@ def check(s, grads, scale=0.5, eps=1e-6):
 
 
 @pytest.mark.parametrize("res,dt", [(BF16, BF16), (F32, BF16), (F32, F32)])
-@pytest.mark.parametrize("n,d", [(1, 1), (3, 7), (2, 64), (5, 255), (130, 257), (7, 768), (33, 1000), (2, 2048), (3, 2049), (9, 4104),
-                                 (1, 5120), (70, 5120), (4, 8192), (2, 8200), (2, 16384), (1, 20001)])
+@pytest.mark.parametrize("n,d", [(1, 1), (3, 3), (3, 7), (2, 8), (2, 64), (5, 255), (130, 257), (7, 768), (33, 1000), (2, 2048), (3, 2049), (9, 4104),
+                                 (1, 5120), (70, 5120), (600, 5123),
+                                 (4, 8192), (2, 8200), (3, 9001), (5, 10240), (300, 10243), (2, 16384), (3, 16391), (2, 19456), (1, 20001)])
 def test_sizes(n, d, res, dt):
     check(*make(n * 100003 + d, n, d, res, dt))
 
