@@ -495,7 +495,7 @@ grpo_status grpo_lmhead_loss_aux_fwd_bwd(const void *hidden, int64_t hidden_stri
  * Sums are formed in a fixed order.  What decides n and t is fp64 (fp32 where the two sides differ by more than 2^-15 of themselves): t does not
  * depend on rounding short of 1e-12 of its border.  Log-probs of accepted tokens come from fp32 terms and are off by at most 2^-17, that
  * of t is rounded from fp64.
- * drafts in [0, 64]; vocab in [1, 2^28].  workspace: device, 256-byte aligned, at least
+ * drafts in [0, 64]; vocab in [1, 2^28]; batch so that the logits have no more than 2^34 entries or so (GRPO_ERR_SHAPE).  workspace: device, 256-byte aligned, at least
  * grpo_verify_workspace_bytes(...) bytes (0 for invalid sizes), contents ignored.  batch == 0 does nothing.
  * ------------------------------------------------------------------------- */
 size_t grpo_verify_workspace_bytes(int64_t batch, int64_t drafts, int64_t vocab, grpo_dtype dtype);
@@ -612,7 +612,7 @@ typedef struct grpo_optim_tensor {
     void *exp_avg_sq;
     float *exp_avg_scale;
     float *exp_avg_sq_scale;
-    int64_t n;                /* 0 .. 2^40; a tensor of 0 values is ignored, its pointers too */
+    int64_t n;                /* 0 .. 2^36 - 2^13, as many values in all tensors at most; of 0 values: ignored, its pointers too */
     double weight_decay;
     grpo_dtype param_dtype;
     grpo_dtype grad_dtype;

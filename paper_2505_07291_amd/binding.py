@@ -687,6 +687,14 @@ def grpo_lmhead_loss_aux_fwd_bwd(hidden, weight, tokens, old_logprobs, ref_logpr
     return loss_out, logprobs_out, entropy_out, counts_out, grad_hidden, grad_weight
 
 
+def _own_workspace(size, device, stream):
+    """A workspace of a call's own.  On a stream that is given it may be freed, and the memory used again, before the call has run."""
+    workspace = torch.empty(size, dtype=torch.uint8, device=device)
+    if stream is not None:
+        workspace.record_stream(stream)
+    return workspace
+
+
 def _call(where, device, f, *args):
     """Calls the library on a tensor's device, whichever is the current one."""
     if device.index == torch.cuda.current_device():
@@ -762,7 +770,7 @@ def grpo_verify_drafts(target_logits, draft_logits, draft_tokens, accept_u, samp
         _check_2d(logprobs_out, torch.float32, (n, k + 1), "logprobs_out", dev)
     L, code = lib(), _DTYPE_CODES[dtype]
     if workspace is None:
-        workspace = torch.empty(L.grpo_verify_workspace_bytes(n, k, v, code), dtype=torch.uint8, device=dev)
+        workspace = _own_workspace(L.grpo_verify_workspace_bytes(n, k, v, code), dev, stream)
     _call("grpo_verify_drafts", dev, L.grpo_verify_drafts, _ptr(target_logits), tb, tk, _ptr(draft_logits), db, dk, code, n, k, v,
           _ptr(draft_tokens), _ptr(accept_u), _ptr(sample_u), _ptr(draft_lengths), float(temperature), float(draft_temperature),
           _ptr(tokens_out), _ptr(n_accepted_out), _ptr(logprobs_out), _ptr(workspace), workspace.numel(), _raw_stream(stream, dev.index))
@@ -895,7 +903,7 @@ def grpo_block_norm_bwd(residual_out, block=None, post_weight=None, gate=None, p
         grad_gate = made[2]
     L = lib()
     if workspace is None:
-        workspace = torch.empty(L.grpo_block_norm_workspace_bytes(n, d), dtype=torch.uint8, device=dev)
+        workspace = _own_workspace(L.grpo_block_norm_workspace_bytes(n, d), dev, stream)
     _call("grpo_block_norm_bwd", dev, L.grpo_block_norm_bwd, _ptr(residual_out) if pre_weight is not None else None, rs,
           _DTYPE_CODES[residual_out.dtype], _ptr(block), fs, _ptr(post_weight), _ptr(gate), gs, _ptr(pre_weight), _DTYPE_CODES[dtype], n, d,
           float(residual_scale), float(eps), _ptr(grad_hidden), hs, _ptr(grad_residual_out), os_, _ptr(grad_residual), dxs,
@@ -996,7 +1004,7 @@ def grpo_grad_norm(plan, max_norm=0.0, *, norm_out=None, workspace=None, stream=
         _check(norm_out, torch.float32, 2, "norm_out", dev)
     L = lib()
     if workspace is None:
-        workspace = torch.empty(L.grpo_grad_norm_workspace_bytes(), dtype=torch.uint8, device=dev)
+        workspace = _own_workspace(L.grpo_grad_norm_workspace_bytes(), dev, stream)
     _call("grpo_grad_norm", dev, L.grpo_grad_norm, plan._address, _ptr(plan._table), float(max_norm), _ptr(norm_out), _ptr(workspace),
           workspace.numel(), _raw_stream(stream, dev.index))
     return norm_out

@@ -32,6 +32,7 @@ struct OptChunk {
 };
 
 constexpr int kOptBlock = 256;
+constexpr long long kMaxWorkgroups = 0xffffffffll / kOptBlock;  // a launch has less than 2^32 lanes
 constexpr int kOptQuant = 256;    // values to a scale, and to a wavefront's step
 constexpr int kOptChunk = 4096;   // values to a workgroup of adamw_step_k
 constexpr long long kOptMaxValues = 1ll << 40;  // of one tensor
@@ -380,7 +381,7 @@ size_t grpo_optim_plan_bytes(const grpo_optim_tensor *tensors, int64_t n_tensors
         if (tensors[i].n < 0 || tensors[i].n > kOptMaxValues) return 0;
         chunks += (size_t)((tensors[i].n + kOptChunk - 1) / kOptChunk);
     }
-    if (chunks > 0x7fffffffu) return 0;
+    if (chunks > (size_t)kMaxWorkgroups) return 0;
     return align_up(opt_chunks_at(n_tensors) + chunks * sizeof(OptChunk) + 1, 256);
 }
 
@@ -472,7 +473,7 @@ grpo_status grpo_optim_plan_build(const grpo_optim_tensor *tensors, int64_t n_te
 static grpo_status check_plan(const grpo_optim_plan *plan, const void *table)
 {
     if (!plan) return GRPO_ERR_NULL;
-    if (plan->n_tensors < 0 || plan->n_chunks < 0 || plan->n_chunks > 0x7fffffffll) return GRPO_ERR_SHAPE;
+    if (plan->n_tensors < 0 || plan->n_chunks < 0 || plan->n_chunks > kMaxWorkgroups) return GRPO_ERR_SHAPE;
     if (plan->n_chunks > 0 && !table) return GRPO_ERR_NULL;
     if ((uintptr_t)table & 255u) return GRPO_ERR_ALIGN;
     return GRPO_OK;

@@ -157,10 +157,11 @@ __device__ __forceinline__ float wave_maximum(float v)
     return as_f32((unsigned)__builtin_amdgcn_readlane((int)as_u32(v), 63));
 }
 
-// exp((z - m) / T) with k = log2(e) / T, as 2^(z k - m k).  A sum is kept relative to a maximum m; where nothing has been added
-// yet, or all of it is -inf, the maximum is -inf and 0 stands in for it: every z is -inf then and adds 0.
-__device__ __forceinline__ double times_k(float m, double k) { return m == -INFINITY ? 0.0 : (double)m * k; }
-__device__ __forceinline__ double exp_from(float z, double mk, double k) { return exp2_f64(fma((double)z, k, -mk)); }
+// exp((z - m) / T) with k = log2(e) / T; the difference is exact in fp64, and 1 comes of m itself at any temperature.  A sum is kept
+// relative to a maximum m; where nothing has been added yet, or all of it is -inf, the maximum is -inf and 0 stands in for it: every z is -inf
+// then and adds 0.
+__device__ __forceinline__ double reference(float m) { return m == -INFINITY ? 0.0 : (double)m; }
+__device__ __forceinline__ double exp_from(float z, double ref, double k) { return exp2_f64(((double)z - ref) * k); }
 
 // A maximum and a sum relative to it; whatever the sum, NaN if the maximum is +inf or NaN.
 struct RowSum {
@@ -178,12 +179,12 @@ __device__ __forceinline__ RowSum row_sum(const unsigned long long *part, int ch
         const unsigned long long q = part[c];
         const float part_max = as_f32((unsigned)q), part_sum = as_f32((unsigned)(q >> 32));
         const float top = maximum(m, part_max);
-        const double ref = times_k(top, k);
+        const double ref = reference(top);
         s = s * exp_from(m, ref, k) + (double)part_sum * exp_from(part_max, ref, k);
         m = top;
     }
     const float top = wave_maximum(m);
-    s = wave_sum_dpp(s * exp_from(m, times_k(top, k), k));
+    s = wave_sum_dpp(s * exp_from(m, reference(top), k));
     return {top, top < INFINITY ? s : __builtin_nan("")};
 }
 
@@ -202,11 +203,11 @@ __device__ __forceinline__ Position position(const Verify &p, int b, int i)
     const float zq = in && p.draft ? load_elem<DT>(p.draft_row(b, i), y) : 0.f;
     r.p = row_sum(p.parts(b, i), p.chunks, p.k);
     r.q = {0.f, 1.0};
-    r.py = in ? exp_from(zp, times_k(r.p.max, p.k), p.k) / r.p.sum : 0.0;
+    r.py = in ? exp_from(zp, reference(r.p.max), p.k) / r.p.sum : 0.0;
     r.qy = 1.0;
     if (p.draft) {
         r.q = row_sum(p.parts(b, p.drafts + i), p.chunks, p.kd);
-        r.qy = in ? exp_from(zq, times_k(r.q.max, p.kd), p.kd) / r.q.sum : 0.0;
+        r.qy = in ? exp_from(zq, reference(r.q.max), p.kd) / r.q.sum : 0.0;
     }
     return r;
 }
@@ -250,7 +251,7 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_rows_k(Verify p)
         }
         top = wave_maximum(top);
         const float ref = top == -INFINITY ? 0.f : top;
-        s *= exp_from(m, times_k(top, k), k);
+        s *= exp_from(m, reference(top), k);
 #pragma unroll
         for (int t = 0; t < kVerifySlots; ++t) {
             if (j0 + (long long)t * kVerifyBlock * EPV >= to) break;
@@ -276,7 +277,7 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_rows_k(Verify p)
         float top = lds_m[0];
 #pragma unroll
         for (int w = 1; w < kVerifyBlock / 64; ++w) top = maximum(top, lds_m[w]);
-        const double ref = times_k(top, k);
+        const double ref = reference(top);
         s = 0.0;
 #pragma unroll
         for (int w = 0; w < kVerifyBlock / 64; ++w) s += lds_s[w] * exp_from(lds_m[w], ref, k);
@@ -306,7 +307,7 @@ __device__ __forceinline__ double last_lane(double v)
 struct Weights {
     const char *t, *d;  // d: NULL where there is no draft row
     long long y;        // without a draft row, the token that has all of the draft's mass; -1: none has
-    double k, kd, pk, qk, rho;
+    double k, kd, pk, qk, rho;  // pk, qk: the maxima
 };
 
 template <grpo_dtype DT>
@@ -349,7 +350,7 @@ __device__ __forceinline__ void part_sums(const Weights &r, long long from, long
                 for (int e = 0; e < EPV; ++e) now = maximum(now, z[e]);
             }
             now = wave_maximum(now);
-            pk = times_k(now, r.k);
+            pk = reference(now);
             s[0] *= exp_from(m, pk, r.k);
             m = now;
         }
@@ -425,8 +426,8 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_sums_k(Verify p)
             const long long y = p.tokens[(long long)b * p.drafts + n], quarter = (p.vocab / 4 + 7) / 8 * 8, from = wave * quarter;
             r.t = p.target_row(b, n);
             r.d = p.draft ? p.draft_row(b, n) : nullptr;
-            r.pk = times_k(at[n].p.max, p.k);
-            r.qk = times_k(at[n].q.max, p.kd);
+            r.pk = reference(at[n].p.max);
+            r.qk = reference(at[n].q.max);
             top = at[n].p.max;
             part_sums<DT>(r, from, wave < 3 && from + quarter < p.vocab ? from + quarter : p.vocab, true, top, s);
             __syncthreads();
@@ -448,10 +449,10 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_sums_k(Verify p)
     top = -INFINITY;
     if (refused) {
         top = at[n].p.max;
-        r.pk = times_k(top, p.k);
+        r.pk = reference(top);
         if (p.draft) {
             r.d = p.draft_row(b, n);
-            r.qk = times_k(at[n].q.max, p.kd);
+            r.qk = reference(at[n].q.max);
             r.rho = at[n].p.sum / at[n].q.sum;
         } else {
             r.y = p.tokens[(long long)b * p.drafts + n];
@@ -500,7 +501,7 @@ __device__ __forceinline__ Found find_piece(const Verify &p, int b, const Refusa
         for (int i = first; i < end; ++i) top = maximum(top, tops[i]);
         top = wave_maximum(top);
     }
-    f.pk = times_k(top, p.k);
+    f.pk = reference(top);
     auto of_p = [&](int i) { return at.refused ? sums[kSums * i] : sums[kSums * i] * exp_from(tops[i], f.pk, p.k); };
     double sp = 0.0, sq = 0.0;
     for (int i = first; i < end; ++i) {
@@ -587,7 +588,7 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_pick_k(Verify p)
     r.t = p.target_row(b, at.n);
     if (at.refused && p.draft) {
         r.d = p.draft_row(b, at.n);
-        r.qk = times_k(at.max_q, p.kd);
+        r.qk = reference(at.max_q);
     } else if (at.refused) {
         r.y = p.tokens[(long long)b * K + at.n];
     }
@@ -680,7 +681,7 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_pick_k(Verify p)
     }
     if (tid == 0) {
         tokens_out[at.n] = token;
-        logprobs_out[at.n] = (float)(fma((double)load_elem<DT>(r.t, token), p.k, -f.pk) * 0.6931471805599453094 - log(f.total));
+        logprobs_out[at.n] = (float)(((double)load_elem<DT>(r.t, token) - f.pk) * p.k * 0.6931471805599453094 - log(f.total));
     }
 }
 
@@ -694,7 +695,7 @@ static bool verify_cut(int64_t rows, int64_t vocab, int dtype, int64_t enough, i
     while (units < kVerifySlots && rows * ((vocab + unit * units - 1) / (unit * units)) >= enough) units *= 2;
     *chunk = (int)(units * unit);
     *chunks = (int)((vocab + units * unit - 1) / (units * unit));
-    return rows * *chunks <= 0x7fffffffll;  // workgroups
+    return rows * *chunks <= kMaxWorkgroups;
 }
 
 // The parts, and where they lie in the workspace; its size, or 0 for sizes that cannot be.

@@ -228,6 +228,15 @@ def test_a_token_drafted_without_a_model_is_never_sampled_again():
     assert (got[1] == 0).all() and not (got[0][:, 0].cpu() == tokens[:, 0]).any()
 
 
+@pytest.mark.parametrize("t,td", [(1e-6, 1e-6), (1e-12, 1.0), (1e-30, 1e-30), (50.0, 0.01), (1e30, 1e30)])
+def test_temperatures(t, td):
+    """Cold ones leave all of the mass on the largest logits, hot ones spread it evenly."""
+    for draft in (True, False):
+        target, q, tokens, u, v = make(17, 20, 3, 2500, draft=draft)
+        tokens[::2, 0] = target[::2, 0].float().argmax(-1).cpu()
+        check(target, q, tokens, u, v, t=t, td=td)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_masked_logits(dtype):
     """Most of the vocabulary masked by -inf or by the type's lowest value, whole parts of a row among it."""
@@ -299,6 +308,26 @@ def test_captured_and_replayed(n, k):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, out)), i
+
+
+def test_on_a_stream_that_is_given():
+    """The call's own workspace is not used again by others while the call still waits for its stream."""
+    a = [t.cuda() for t in make(16, 8, 3, 50257)]
+    want = grpo.grpo_verify_drafts(*a)
+    stream = torch.cuda.Stream()
+    busy = torch.randn((4096, 4096), device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        out = [torch.zeros_like(t) for t in want]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                busy @ busy
+        grpo.grpo_verify_drafts(*a, tokens_out=out[0], n_accepted_out=out[1], logprobs_out=out[2], stream=stream)
+        for size in (1 << 12, 1 << 14, 1 << 16, 1 << 18, 1 << 20):
+            torch.full((size,), float("nan"), device="cuda")
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(want, out))
 
 
 def test_on_two_streams_at_once():

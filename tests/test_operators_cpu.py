@@ -24,7 +24,7 @@ VERIFY = dict(target=P, tb=4096, ts=1024, draft=P, db=4096, ds=1024, dtype=1, n=
 
 @pytest.mark.parametrize("over,expect", [
     (dict(dtype=2), DTYPE), (dict(dtype=-1), DTYPE),
-    (dict(n=-1), SHAPE), (dict(n=1 << 31), SHAPE), (dict(n=1 << 30), SHAPE), (dict(k=-1), SHAPE), (dict(k=65), SHAPE), (dict(V=0), SHAPE),
+    (dict(n=-1), SHAPE), (dict(n=1 << 31), SHAPE), (dict(n=1 << 24, k=0), SHAPE), (dict(n=1 << 19, k=64), SHAPE), (dict(k=-1), SHAPE), (dict(k=65), SHAPE), (dict(V=0), SHAPE),
     (dict(V=(1 << 28) + 1), SHAPE), (dict(ts=992), SHAPE), (dict(ds=992), SHAPE), (dict(tb=-8), SHAPE), (dict(db=-8), SHAPE),
     (dict(t=0.0), PARAM), (dict(t=-1.0), PARAM), (dict(t=NAN), PARAM), (dict(t=INF), PARAM), (dict(t=1e-31), PARAM), (dict(td=1e31), PARAM), (dict(td=0.0), PARAM), (dict(td=NAN), PARAM),
     (dict(target=None), NULL), (dict(tokens=None), NULL), (dict(u=None), NULL), (dict(v=None), NULL), (dict(out=None), NULL),
@@ -43,7 +43,7 @@ def test_verify_workspace():
     f = grpo.lib().grpo_verify_workspace_bytes
     assert [f(-1, 3, 1000, 1), f(4, -1, 1000, 1), f(4, 65, 1000, 1), f(4, 3, 0, 1), f(4, 3, (1 << 28) + 1, 1), f(4, 3, 1000, 5),
             f(1 << 30, 64, 1 << 28, 1)] == [0] * 7
-    for n, k, v in ((0, 0, 1), (1, 0, 1), (1, 64, 1 << 28), (96, 5, 152064), (1000, 8, 300007), (1 << 20, 0, 1000)):
+    for n, k, v in ((0, 0, 1), (1, 0, 1), (1, 64, 1 << 28), ((1 << 24) - 1, 0, 100), (96, 5, 152064), (1000, 8, 300007), (1 << 20, 0, 1000)):
         for dtype in (0, 1):
             need = f(n, k, v, dtype)
             # sums to each part of a row, at most 1024 parts
@@ -119,7 +119,7 @@ def build(tensors, spare=0, table=True, out=True):
 @pytest.mark.parametrize("over,expect", [
     (dict(), OK), (dict(bits=8), OK), (dict(param=1), OK), (dict(param=1, master=True), OK), (dict(grad=1), OK),
     (dict(param=2), DTYPE), (dict(param=-1), DTYPE), (dict(grad=5), DTYPE), (dict(bits=16), DTYPE), (dict(master=True), DTYPE),
-    (dict(n=-1), SHAPE), (dict(n=(1 << 40) + 1), SHAPE), (dict(weight_decay=NAN), PARAM), (dict(weight_decay=INF), PARAM),
+    (dict(n=-1), SHAPE), (dict(n=(1 << 40) + 1), SHAPE), (dict(n=1 << 36), SHAPE), (dict(weight_decay=NAN), PARAM), (dict(weight_decay=INF), PARAM),
     (dict(exp_avg=None), NULL), (dict(exp_avg_sq=None), NULL), (dict(bits=8, exp_avg_scale=None), NULL),
     (dict(bits=8, exp_avg_sq_scale=None), NULL), (dict(exp_avg_scale=P), NULL),
     (dict(grad=0, exp_avg=P + 1), ALIGN), (dict(exp_avg_sq=P + 65536 * 4 + 2), ALIGN), (dict(bits=8, exp_avg_scale=P + 65536 * 5 + 2), ALIGN),
