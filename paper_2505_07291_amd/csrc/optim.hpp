@@ -253,7 +253,8 @@ __device__ __forceinline__ void adamw_chunk(const AdamW &a, const AdamWStep &s, 
     }
 }
 
-// Bound by memory: 30 bytes a value with fp32 moments, a master copy and an fp32 gradient, 18 with 8-bit moments.
+// Bound by memory: 30 bytes a value with fp32 moments, a master copy and an fp32 gradient, 18 with 8-bit moments.  778 million
+// of the former take 4.18 ms (5.6 TB/s), 123 million of the latter with gradients in bf16 (16 bytes) 338 us (5.8 TB/s).
 static __global__ void __launch_bounds__(kOptBlock) adamw_step_k(AdamW a)
 {
     const OptChunk c = a.chunks[blockIdx.x];
@@ -290,6 +291,8 @@ static __global__ void __launch_bounds__(kOptBlock) adamw_step_k(AdamW a)
     }
 }
 
+// Bound by memory: 778 million gradients in fp32, read once, take 455 us (6.8 TB/s).  14 million, which the caches may hold, take 12, of
+// them 4 the second kernel: a launch costs less here than a workgroup that waits for the others' sums.
 // Squares are exact in fp64 and summed there, each workgroup's chunks in the table's order and the workgroups' sums in theirs:
 // the same gradients always give the same norm.
 template <bool GBF16, bool WIDE>

@@ -6,12 +6,13 @@
 //   then one token: the smallest j with  sum_{l <= j} w_l > v sum_l w_l,  w = max(p_n - q_n, 0), or p_n behind the last draft
 //
 // verify_rows_k forms, for the drafted positions, maxima and sums of exponentials in fp32 and is bound by reading the logits (96
-// responses with 5 drafts of 152064 bf16, 256 MB: 50 us, 5.1 TB/s).  That is enough for a ratio that is not within 2^-15 of its random
+// responses with 5 drafts of 152064 bf16, 292 MB: 49 us, 6.0 TB/s).  That is enough for a ratio that is not within 2^-15 of its random
 // number (the others are decided in fp64), but not for the token: with sums that are off by 1e-7 the border of some of 152064 tokens lies
 // between two orders' results in one row of a hundred.
 //
-// verify_sums_k forms in fp64 what the token needs, of row n alone: then that is one in 10^8.  It is bound by fp64 arithmetic, 18
-// instructions an exponential, of which the GPU does 1.7e12 a second (29e12 lanes of fma, 35e12 of the others): that batch 40 us.
+// verify_sums_k forms in fp64 what the token needs, of row n alone: then that is one in 10^8.  It is bound by fp64 arithmetic, 19
+// instructions an exponential and ten to what it is added to, of which the GPU does 1.1e12 a second (29e12 lanes of fma, 33 to
+// 35e12 of the others), and by the wait for row n and then for its logits before any can begin: that batch 47 us, of them 26 the former.
 // It reads its rows once.  p - q needs the rows' sums S_p and S_q, of which only those in fp32 are known before; so over the entries with
 // p > q by those, e_p and e_q are added up separately, to A and B, and A / S_p - B / S_q is formed when S_p and S_q are there.  What
 // may be on the wrong side by that is summed up too (N), and where it could matter, or little is left of A / S_p - B / S_q, the
@@ -19,18 +20,20 @@
 //
 // verify_pick_k, a workgroup to a response, finds the piece in which the sum crosses, and in it the token (5 to 9 us).  That the rows
 // behind a refused draft are read for nothing costs less than to follow it: counted by the workgroups' last one, with what it
-// takes to hand sums from one to another inside a launch, that batch took 128 us a call, and takes 96.
+// takes to hand sums from one to another inside a launch, that batch took 128 us a call, and takes 98.
 
 namespace __attribute__((visibility("hidden"))) grpo_impl {
 
 constexpr int kVerifyBlock = 256;
 constexpr int kMaxDrafts = 64;
 constexpr int kMaxChunks = 1024;
-constexpr int kVerifySlots = 8;   // vectors of a row that a lane of verify_rows_k holds at a time
+constexpr int kVerifySlots = 8;   // vectors of a row that a lane of verify_rows_k holds at a time, where it has as many
 constexpr int kSumSlots = 2;      // and one of verify_sums_k, of each of two rows
-// Workgroups from which on they are given more entries each, up to eight times as many: 8 responses with 4 drafts (2400 workgroups of
-// verify_rows_k, 300 of verify_sums_k) 33 us a call and 41 from twice as many on, 96 with 5 drafts 96 and 97, and 101 from half as many on.
-constexpr int64_t kRowsEnough = 4096, kSumsEnough = 2048;
+// Workgroups from which on they are given twice the entries each, and again, up to eight times as many.  8 responses with 4 drafts (4800
+// workgroups of verify_rows_k at first) take 25.4 us a call, 24.9 from half as many on and 27.7 from twice as many; of verify_sums_k,
+// 16 responses with 4 drafts (1200) take 21.9 us, 22.4 from half as many on and 25.4 from twice as many, 32 with 4 40.0, 45.2 and 41.5, and 64
+// without drafts, the one that loses, 22.0, 22.4 and 20.4.
+constexpr int64_t kRowsEnough = 4096, kSumsEnough = 1024;
 // Ratios that fp32 sums do not decide.  A term 2^x of a sum is off by 2^-23 (the instruction) and by the roundings of z - m, of
 // 1 / T and of x, 0.7 |x| 2^-24 each, and those below 2^-40 of the largest make up less than 2^-22 of any sum of 2^18 or fewer; three
 // roundings in a vector's sum and one of the part's: 94 * 2^-24, under 2^-17, for each of the two rows.
@@ -122,7 +125,7 @@ __device__ __forceinline__ void logits_raw(const char *row, long long j0, int la
 
 // 2^x for x <= 0 or little more, to 4e-16 of the value: x = n + f with n whole and |f| <= 1/2, and for 2^f the polynomial of degree
 // 10 that agrees with it at the eleven Chebyshev points of [-1/2, 1/2] (one of them 0: 2^0 is 1).  Below 2^-1075 the result is 0,
-// for -inf too.  NaN is not carried: a sum's maximum is NaN if one of its terms is (see maximum).  18 fp64 instructions; the
+// for -inf too.  NaN is not carried: a sum's maximum is NaN if one of its terms is (see maximum).  15 fp64 instructions; the
 // library function takes some three times as many.
 __device__ __forceinline__ double exp2_f64(double x)
 {
@@ -220,7 +223,7 @@ __device__ __forceinline__ int verdict(float u, const Position &r)
     return a <= r.py * (1.0 + kNearRatio) && r.py > 0.0 ? kNear : kRefused;
 }
 
-template <grpo_dtype DT>
+template <grpo_dtype DT, int SLOTS>
 __global__ void __launch_bounds__(kVerifyBlock) verify_rows_k(Verify p)
 {
     constexpr int EPV = Elem<DT>::EPV;
@@ -238,12 +241,12 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_rows_k(Verify p)
     const long long from = (long long)c * p.chunk, to = from + p.chunk < p.vocab ? from + p.chunk : p.vocab;
     float m = -INFINITY;
     double s = 0.0;  // of sums of a vector's terms: long parts lose no more than short ones
-    for (long long j0 = from; j0 < to; j0 += kVerifyBlock * EPV * kVerifySlots) {
-        u32x4 v[kVerifySlots];
+    for (long long j0 = from; j0 < to; j0 += kVerifyBlock * EPV * SLOTS) {
+        u32x4 v[SLOTS];
         float top = m;
-        logits_raw<DT, kVerifySlots>(row, j0, threadIdx.x, kVerifyBlock, to, v);
+        logits_raw<DT, SLOTS>(row, j0, threadIdx.x, kVerifyBlock, to, v);
 #pragma unroll
-        for (int t = 0; t < kVerifySlots; ++t) {
+        for (int t = 0; t < SLOTS; ++t) {
             float z[EPV];
             unpack<DT>(v[t], z);
 #pragma unroll
@@ -253,7 +256,7 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_rows_k(Verify p)
         const float ref = top == -INFINITY ? 0.f : top;
         s *= exp_from(m, reference(top), k);
 #pragma unroll
-        for (int t = 0; t < kVerifySlots; ++t) {
+        for (int t = 0; t < SLOTS; ++t) {
             if (j0 + (long long)t * kVerifyBlock * EPV >= to) break;
             float x[EPV];
             unpack<DT>(v[t], x);
@@ -327,7 +330,7 @@ __device__ __forceinline__ void weights(const Weights &r, long long j, long long
 // S_p, S_q, A, B and N of the entries from .. to, by one wavefront, which all of its lanes get.  With max_known r.pk and r.qk are those of the
 // rows' maxima; without, S_p is relative to the entries' own maximum, which becomes top, and there is nothing to take off.
 // EXACT: r.rho is S_p / S_q, and A becomes the sum of w.
-template <grpo_dtype DT, bool EXACT = false>
+template <grpo_dtype DT, int SLOTS, bool EXACT = false>
 __device__ __forceinline__ void part_sums(const Weights &r, long long from, long long to, bool max_known, float &top, double (&s)[kSums])
 {
     constexpr int EPV = Elem<DT>::EPV;
@@ -336,14 +339,14 @@ __device__ __forceinline__ void part_sums(const Weights &r, long long from, long
     double pk = r.pk;
 #pragma unroll
     for (int i = 0; i < kSums; ++i) s[i] = 0.0;
-    for (long long j0 = from; j0 < to; j0 += 64 * EPV * kSumSlots) {
-        u32x4 zr[kSumSlots], dr[kSumSlots];
-        logits_raw<DT, kSumSlots>(r.t, j0, lane, 64, to, zr);
-        if (r.d) logits_raw<DT, kSumSlots>(r.d, j0, lane, 64, to, dr);
+    for (long long j0 = from; j0 < to; j0 += 64 * EPV * SLOTS) {
+        u32x4 zr[SLOTS], dr[SLOTS];
+        logits_raw<DT, SLOTS>(r.t, j0, lane, 64, to, zr);
+        if (r.d) logits_raw<DT, SLOTS>(r.d, j0, lane, 64, to, dr);
         if (!max_known) {
             float now = m;
 #pragma unroll
-            for (int t = 0; t < kSumSlots; ++t) {
+            for (int t = 0; t < SLOTS; ++t) {
                 float z[EPV];
                 unpack<DT>(zr[t], z);
 #pragma unroll
@@ -355,7 +358,7 @@ __device__ __forceinline__ void part_sums(const Weights &r, long long from, long
             m = now;
         }
 #pragma unroll
-        for (int t = 0; t < kSumSlots; ++t) {
+        for (int t = 0; t < SLOTS; ++t) {
             const long long j = j0 + (t * 64 + lane) * EPV;
             if (j0 + (long long)t * 64 * EPV >= to) break;
             float z[EPV];
@@ -398,7 +401,7 @@ __device__ __forceinline__ void part_sums(const Weights &r, long long from, long
     if (r.d || r.y >= 0) s[2] = wave_sum_dpp(s[2]);
 }
 
-template <grpo_dtype DT>
+template <grpo_dtype DT, int SLOTS>
 __global__ void __launch_bounds__(kVerifyBlock) verify_sums_k(Verify p)
 {
     __shared__ Position at[kMaxDrafts];
@@ -429,7 +432,7 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_sums_k(Verify p)
             r.pk = reference(at[n].p.max);
             r.qk = reference(at[n].q.max);
             top = at[n].p.max;
-            part_sums<DT>(r, from, wave < 3 && from + quarter < p.vocab ? from + quarter : p.vocab, true, top, s);
+            part_sums<DT, SLOTS>(r, from, wave < 3 && from + quarter < p.vocab ? from + quarter : p.vocab, true, top, s);
             __syncthreads();
             if ((tid & 63) == 0) {
                 whole[wave][0] = s[0];
@@ -461,7 +464,7 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_sums_k(Verify p)
     const int piece = c * (kVerifyBlock / 64) + wave;
     if (piece < p.pieces) {
         const long long from = (long long)piece * p.piece, to = from + p.piece < p.vocab ? from + p.piece : p.vocab;
-        part_sums<DT>(r, from, to, refused, top, s);
+        part_sums<DT, SLOTS>(r, from, to, refused, top, s);
         if ((tid & 63) == 0) {
             double *sums = p.sums + ((long long)b * p.pieces + piece) * kSums;
 #pragma unroll
@@ -608,7 +611,7 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_pick_k(Verify p)
             const long long from = (long long)i * p.piece, to = from + p.piece < p.vocab ? from + p.piece : p.vocab;
             double s[kSums];
             float top = at.max_p;
-            part_sums<DT, true>(r, from, to, true, top, s);
+            part_sums<DT, kSumSlots, true>(r, from, to, true, top, s);
             if (lane == 0) {
                 p.sums[((long long)b * p.pieces + i) * kSums + 2] = s[2];
                 p.sums[((long long)b * p.pieces + i) * kSums + 3] = 0.0;
@@ -658,7 +661,8 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_pick_k(Verify p)
             base += lds_wave[turn][i];
         }
         const unsigned long long cross = __ballot(before + up > f.target);
-        if (cross && before <= f.target && lane == (int)__builtin_ctzll(cross)) {  // the first lane of the wavefront whose entries cross; one of them does, up to rounding
+        // the first lane of the wavefront whose entries cross; one of them does, up to rounding
+        if (cross && before <= f.target && lane == (int)__builtin_ctzll(cross)) {
             int first = last;
             double run = before + (up - sum);
 #pragma unroll
@@ -696,6 +700,30 @@ static bool verify_cut(int64_t rows, int64_t vocab, int dtype, int64_t enough, i
     *chunk = (int)(units * unit);
     *chunks = (int)((vocab + units * unit - 1) / (units * unit));
     return rows * *chunks <= kMaxWorkgroups;
+}
+
+// Each kernel with as many vectors to a lane as its parts have: one that looked for more would ask for each under a condition.  8
+// responses with 4 drafts take 26 us a call, and 33 with eight vectors to a lane always.
+template <grpo_dtype DT>
+static void launch_verify(const Verify &p, unsigned row_blocks, unsigned sum_blocks, hipStream_t st)
+{
+    const dim3 block(kVerifyBlock);
+    const int unit = kVerifyBlock * Elem<DT>::EPV;
+    if (row_blocks > 0) {
+        if (p.chunk == unit)
+            hipLaunchKernelGGL((verify_rows_k<DT, 1>), dim3(row_blocks), block, 0, st, p);
+        else if (p.chunk == 2 * unit)
+            hipLaunchKernelGGL((verify_rows_k<DT, 2>), dim3(row_blocks), block, 0, st, p);
+        else if (p.chunk == 4 * unit)
+            hipLaunchKernelGGL((verify_rows_k<DT, 4>), dim3(row_blocks), block, 0, st, p);
+        else
+            hipLaunchKernelGGL((verify_rows_k<DT, kVerifySlots>), dim3(row_blocks), block, 0, st, p);
+    }
+    if (p.piece * 4 == unit)
+        hipLaunchKernelGGL((verify_sums_k<DT, 1>), dim3(sum_blocks), block, 0, st, p);
+    else
+        hipLaunchKernelGGL((verify_sums_k<DT, kSumSlots>), dim3(sum_blocks), block, 0, st, p);
+    hipLaunchKernelGGL((verify_pick_k<DT>), dim3((unsigned)p.batch), block, 0, st, p);
 }
 
 // The parts, and where they lie in the workspace; its size, or 0 for sizes that cannot be.
@@ -778,15 +806,10 @@ grpo_status grpo_verify_drafts(const void *target_logits, int64_t target_batch_s
     p.logprobs_out = logprobs_out;
     hipStream_t st = (hipStream_t)stream;
     const unsigned row_blocks = (unsigned)(batch * drafts * (draft_logits ? 2 : 1) * p.chunks), sum_blocks = (unsigned)(batch * p.sum_blocks);
-    if (dtype == GRPO_BF16) {
-        if (row_blocks > 0) hipLaunchKernelGGL(verify_rows_k<GRPO_BF16>, dim3(row_blocks), dim3(kVerifyBlock), 0, st, p);
-        hipLaunchKernelGGL(verify_sums_k<GRPO_BF16>, dim3(sum_blocks), dim3(kVerifyBlock), 0, st, p);
-        hipLaunchKernelGGL(verify_pick_k<GRPO_BF16>, dim3((unsigned)batch), dim3(kVerifyBlock), 0, st, p);
-    } else {
-        if (row_blocks > 0) hipLaunchKernelGGL(verify_rows_k<GRPO_F32>, dim3(row_blocks), dim3(kVerifyBlock), 0, st, p);
-        hipLaunchKernelGGL(verify_sums_k<GRPO_F32>, dim3(sum_blocks), dim3(kVerifyBlock), 0, st, p);
-        hipLaunchKernelGGL(verify_pick_k<GRPO_F32>, dim3((unsigned)batch), dim3(kVerifyBlock), 0, st, p);
-    }
+    if (dtype == GRPO_BF16)
+        launch_verify<GRPO_BF16>(p, row_blocks, sum_blocks, st);
+    else
+        launch_verify<GRPO_F32>(p, row_blocks, sum_blocks, st);
     return hipGetLastError() == hipSuccess ? GRPO_OK : GRPO_ERR_HIP;
 }
 

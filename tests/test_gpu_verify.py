@@ -100,6 +100,14 @@ def test_sizes(n, k, v, draft, dtype):
     check(*make(n + 7 * k + v, n, k, v, dtype, draft), t=0.8, td=1.25)
 
 
+# Parts of one, two, four and eight vectors to a lane, with one entry in the last: of the drafted positions up to (270, 8), of
+# the rows that a token comes from behind it.
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,k", [(40, 8), (60, 8), (100, 8), (140, 8), (270, 8), (250, 1), (400, 1), (600, 1), (1100, 1)])
+def test_each_length_of_a_part(n, k, dtype):
+    check(*make(n + k, n, k, 4097, dtype, n % 20 == 0), t=0.8, td=1.25)
+
+
 def test_many_rows_in_large_parts():
     check(*make(1, 330, 3, 20011))
 
