@@ -11,16 +11,16 @@
 // between two orders' results in one row of a hundred.
 //
 // verify_sums_k forms in fp64 what the token needs, of row n alone: then that is one in 10^8.  It is bound by fp64 arithmetic, 19
-// instructions an exponential and ten to what it is added to, of which the GPU does 1.1e12 a second (29e12 lanes of fma, 33 to
-// 35e12 of the others), and by the wait for row n and then for its logits before any can begin: that batch 47 us, of them 26 the former.
-// It reads its rows once.  p - q needs the rows' sums S_p and S_q, of which only those in fp32 are known before; so over the entries with
-// p > q by those, e_p and e_q are added up separately, to A and B, and A / S_p - B / S_q is formed when S_p and S_q are there.  What
-// may be on the wrong side by that is summed up too (N), and where it could matter, or little is left of A / S_p - B / S_q, the
-// sums are formed again with the ratio of S_p and S_q as it is.
+// instructions an exponential and five to what it is added to, of which the GPU does 1.3e12 a second (29e12 lanes of fma, 33 to
+// 35e12 of the others), and by the wait for row n and then for its logits before any can begin: that batch 40 us, of them 22 the former.
+// It reads its rows once.  p - q needs the rows' sums S_p and S_q, of which only those in fp32 are known before, rho_0 = S_p / S_q by
+// them.  So W = sum of max(e_p - rho_0 e_q, 0) is formed, and B, the sum of e_q where that is positive; with rho, the ratio as it is, W +
+// (rho_0 - rho) B is S_p times the sum of max(p - q, 0), but for entries that are on the wrong side by rho_0.  How much those
+// can be is summed up too (N), and where it could matter, or little is left of W, the sums are formed again with rho.
 //
 // verify_pick_k, a workgroup to a response, finds the piece in which the sum crosses, and in it the token (5 to 9 us).  That the rows
 // behind a refused draft are read for nothing costs less than to follow it: counted by the workgroups' last one, with what it
-// takes to hand sums from one to another inside a launch, that batch took 128 us a call, and takes 98.
+// takes to hand sums from one to another inside a launch, that batch took 128 us a call, and takes 92.
 
 namespace __attribute__((visibility("hidden"))) grpo_impl {
 
@@ -28,7 +28,7 @@ constexpr int kVerifyBlock = 256;
 constexpr int kMaxDrafts = 64;
 constexpr int kMaxChunks = 1024;
 constexpr int kVerifySlots = 8;   // vectors of a row that a lane of verify_rows_k holds at a time, where it has as many
-constexpr int kSumSlots = 2;      // and one of verify_sums_k, of each of two rows
+constexpr int kSumSlots = 2;      // and one of verify_sums_k
 // Workgroups from which on they are given twice the entries each, and again, up to eight times as many.  8 responses with 4 drafts (4800
 // workgroups of verify_rows_k at first) take 25.4 us a call, 24.9 from half as many on and 27.7 from twice as many; of verify_sums_k,
 // 16 responses with 4 drafts (1200) take 21.9 us, 22.4 from half as many on and 25.4 from twice as many, 32 with 4 40.0, 45.2 and 41.5, and 64
@@ -46,7 +46,7 @@ constexpr int kSums = 5;
 struct Refusal {
     int n, refused;
     float max_p, max_q;
-    double rho;  // S_p / S_q by the sums in fp32
+    double rho;  // rho_0: S_p / S_q by the sums in fp32
 };
 
 struct Verify {
@@ -62,8 +62,8 @@ struct Verify {
     int pieces, piece, sum_blocks;  // verify_sums_k: pieces of row n, each a wavefront's, and entries in one; workgroups to a response
     double k, kd;                   // log2(e) / T, of the target and of the draft
     unsigned long long *part;       // [batch][2 drafts][chunks]: target rows, then draft rows; maximum, and sum of exp((z - maximum) / T)
-    double *sums;                   // [batch][pieces][kSums]: S_p, S_q, A, B, N of a piece of row n
-    float *tops;                    // [batch][pieces]: the maximum that S_p and A are relative to
+    double *sums;                   // [batch][pieces][kSums]: S_p, S_q, W, B, N of a piece of row n
+    float *tops;                    // [batch][pieces]: the maximum that S_p and W are relative to
     Refusal *refusal;               // [batch]
     long long *tokens_out;
     int *accepted_out;
@@ -327,22 +327,18 @@ __device__ __forceinline__ void weights(const Weights &r, long long j, long long
     for (int e = 0; e < EPV; ++e) w[e] = fmax(fma(-r.rho, exp_from(z[e], r.qk, r.kd), w[e]), 0.0);
 }
 
-// S_p, S_q, A, B and N of the entries from .. to, by one wavefront, which all of its lanes get.  With max_known r.pk and r.qk are those of the
-// rows' maxima; without, S_p is relative to the entries' own maximum, which becomes top, and there is nothing to take off.
-// EXACT: r.rho is S_p / S_q, and A becomes the sum of w.
-template <grpo_dtype DT, int SLOTS, bool EXACT = false>
-__device__ __forceinline__ void part_sums(const Weights &r, long long from, long long to, bool max_known, float &top, double (&s)[kSums])
+// S_p, S_q, W, B and N of what a lane has of the entries from .. to; DRAFT: r.d is there.  With max_known S_p and W are relative to r.pk;
+// without, to the entries' own maximum m, and there is nothing to take off.  N: an entry is on the wrong side by rho_0 by less than
+// |rho / rho_0 - 1| e_p - |w|, for a ratio that is off by no more than kNearSide at most that times max(e_p - |w| / kNearSide, 0).
+// Asking for the next entries before these are added up takes 3 us off the batch of 96, one vector at a time where there are two rows
+// another 3.
+template <grpo_dtype DT, int SLOTS, bool EXACT, bool DRAFT>
+__device__ __forceinline__ void lane_sums(const Weights &r, long long from, long long to, bool max_known, float &m, double (&s)[kSums])
 {
-    constexpr int EPV = Elem<DT>::EPV;
+    constexpr int EPV = Elem<DT>::EPV, GROUP = 64 * EPV * SLOTS;
     const int lane = threadIdx.x & 63;
-    float m = -INFINITY;
     double pk = r.pk;
-#pragma unroll
-    for (int i = 0; i < kSums; ++i) s[i] = 0.0;
-    for (long long j0 = from; j0 < to; j0 += 64 * EPV * SLOTS) {
-        u32x4 zr[SLOTS], dr[SLOTS];
-        logits_raw<DT, SLOTS>(r.t, j0, lane, 64, to, zr);
-        if (r.d) logits_raw<DT, SLOTS>(r.d, j0, lane, 64, to, dr);
+    const auto add = [&](const u32x4 (&zr)[SLOTS], const u32x4 (&dr)[SLOTS], long long j0, bool whole) {
         if (!max_known) {
             float now = m;
 #pragma unroll
@@ -360,7 +356,7 @@ __device__ __forceinline__ void part_sums(const Weights &r, long long from, long
 #pragma unroll
         for (int t = 0; t < SLOTS; ++t) {
             const long long j = j0 + (t * 64 + lane) * EPV;
-            if (j0 + (long long)t * 64 * EPV >= to) break;
+            if (!whole && j0 + (long long)t * 64 * EPV >= to) break;
             float z[EPV];
             double ep[EPV];
             unpack<DT>(zr[t], z);
@@ -369,19 +365,17 @@ __device__ __forceinline__ void part_sums(const Weights &r, long long from, long
                 ep[e] = exp_from(z[e], pk, r.k);
                 s[0] += ep[e];
             }
-            if (r.d) {
+            if constexpr (DRAFT) {
                 unpack<DT>(dr[t], z);
 #pragma unroll
                 for (int e = 0; e < EPV; ++e) {
                     const double eq = exp_from(z[e], r.qk, r.kd);
                     s[1] += eq;
                     const double w = fma(-r.rho, eq, ep[e]);
-                    if constexpr (EXACT) {
-                        s[2] += fmax(w, 0.0);
-                    } else {
-                        s[2] += w > 0.0 ? ep[e] : 0.0;
+                    s[2] += fmax(w, 0.0);
+                    if constexpr (!EXACT) {
                         s[3] += w > 0.0 ? eq : 0.0;
-                        s[4] += fabs(w) <= kNearSide * ep[e] ? ep[e] : 0.0;
+                        s[4] += fmax(fma(-1.0 / kNearSide, fabs(w), ep[e]), 0.0);
                     }
                 }
             } else if (r.y >= 0) {
@@ -389,7 +383,52 @@ __device__ __forceinline__ void part_sums(const Weights &r, long long from, long
                 for (int e = 0; e < EPV; ++e) s[2] += j + e == r.y ? 0.0 : ep[e];
             }
         }
+    };
+    u32x4 zr[SLOTS], dr[SLOTS];
+    const int groups = (int)((to - from) / GROUP);
+    if (groups > 0) {  // the next one is asked for before this one is added up; behind the last, the last again
+        const char *zp = r.t + (from + lane * EPV) * Elem<DT>::BYTES, *dp = DRAFT ? r.d + (from + lane * EPV) * Elem<DT>::BYTES : nullptr;
+#pragma unroll
+        for (int t = 0; t < SLOTS; ++t) {
+            zr[t] = *(const u32x4 *)(zp + t * 1024);
+            if constexpr (DRAFT) dr[t] = *(const u32x4 *)(dp + t * 1024);
+        }
+#pragma unroll 1
+        for (int g = 0; g < groups; ++g) {
+            u32x4 zn[SLOTS], dn[SLOTS];
+            const long long next = (long long)(g + 1 < groups ? g + 1 : g) * (GROUP * Elem<DT>::BYTES);
+#pragma unroll
+            for (int t = 0; t < SLOTS; ++t) {
+                zn[t] = *(const u32x4 *)(zp + next + t * 1024);
+                if constexpr (DRAFT) dn[t] = *(const u32x4 *)(dp + next + t * 1024);
+            }
+            add(zr, dr, from + (long long)g * GROUP, true);
+#pragma unroll
+            for (int t = 0; t < SLOTS; ++t) {
+                zr[t] = zn[t];
+                if constexpr (DRAFT) dr[t] = dn[t];
+            }
+        }
     }
+    const long long rest = from + (long long)groups * GROUP;
+    if (rest < to) {
+        logits_raw<DT, SLOTS>(r.t, rest, lane, 64, to, zr);
+        if constexpr (DRAFT) logits_raw<DT, SLOTS>(r.d, rest, lane, 64, to, dr);
+        add(zr, dr, rest, false);
+    }
+}
+
+// The same by one wavefront, which all of its lanes get, and top = m.  EXACT: r.rho is S_p / S_q.
+template <grpo_dtype DT, int SLOTS, bool EXACT = false>
+__device__ __forceinline__ void part_sums(const Weights &r, long long from, long long to, bool max_known, float &top, double (&s)[kSums])
+{
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kSums; ++i) s[i] = 0.0;
+    if (r.d)
+        lane_sums<DT, 1, EXACT, true>(r, from, to, max_known, m, s);
+    else
+        lane_sums<DT, SLOTS, EXACT, false>(r, from, to, max_known, m, s);
     if (!max_known) top = m;
     s[0] = wave_sum_dpp(s[0]);
     if (!(top < INFINITY)) s[0] = __builtin_nan("");
@@ -520,7 +559,7 @@ __device__ __forceinline__ Found find_piece(const Verify &p, int b, const Refusa
     if (!whole) {
         f.rho = r.d ? f.total / sq : 0.0;
         w = 0.0;
-        for (int i = first; i < end; ++i) w += fmax(fma(-f.rho, sums[kSums * i + 3], sums[kSums * i + 2]), 0.0);
+        for (int i = first; i < end; ++i) w += fmax(fma(at.rho - f.rho, sums[kSums * i + 3], sums[kSums * i + 2]), 0.0);
         up = wave_scan(w);
         all = last_lane(up);
         if (r.d && !exact) {
@@ -550,7 +589,7 @@ __device__ __forceinline__ Found find_piece(const Verify &p, int b, const Refusa
     double base = run;
     if (lane == owner)
         for (int i = first; i < end; ++i) {
-            const double x = whole ? of_p(i) : fmax(fma(-f.rho, sums[kSums * i + 3], sums[kSums * i + 2]), 0.0);
+            const double x = whole ? of_p(i) : fmax(fma(at.rho - f.rho, sums[kSums * i + 3], sums[kSums * i + 2]), 0.0);
             if (x > 0.0) {
                 piece = i;
                 base = run;
