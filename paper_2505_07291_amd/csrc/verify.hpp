@@ -299,6 +299,13 @@ __device__ __forceinline__ double wave_scan(double v)
     v += dpp_move<0x143, 0xc>(v);
     return v;
 }
+// The lane in which scanned sums cross, of those that have any.  The scan adds lanes up in different orders: a sum may cross by a
+// rounding in a lane that has nothing, and then it is the last one before it.  Without a crossing, the last that has any.
+__device__ __forceinline__ int crossing(unsigned long long cross, unsigned long long any)
+{
+    const unsigned long long upto = cross ? any & ((cross & -cross) * 2 - 1) : any;
+    return 63 - __builtin_clzll(upto ? upto : any);
+}
 __device__ __forceinline__ double last_lane(double v)
 {
     const long long b = __builtin_bit_cast(long long, v);
@@ -582,8 +589,7 @@ __device__ __forceinline__ Found find_piece(const Verify &p, int b, const Refusa
     }
     f.target = p.v[b] * all;
     // the first lane whose pieces cross, or, where the number is next to 1 and rounding keeps the sum, the last that has any
-    const unsigned long long cross = __ballot(up > f.target), any = __ballot(w > 0.0);
-    const int owner = cross ? __builtin_ctzll(cross) : 63 - __builtin_clzll(any);
+    const int owner = crossing(__ballot(up > f.target), __ballot(w > 0.0));
     double run = up - w;
     int piece = -1;
     double base = run;
@@ -592,7 +598,7 @@ __device__ __forceinline__ Found find_piece(const Verify &p, int b, const Refusa
             const double x = whole ? of_p(i) : fmax(fma(at.rho - f.rho, sums[kSums * i + 3], sums[kSums * i + 2]), 0.0);
             if (x > 0.0) {
                 piece = i;
-                base = run;
+                base = fmin(run, f.target);  // (up - w of this lane may be above the up of the one before it)
             }
             run += x;
             if (run > f.target) break;
@@ -699,11 +705,11 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_pick_k(Verify p)
             if (i < wave) before += lds_wave[turn][i];
             base += lds_wave[turn][i];
         }
-        const unsigned long long cross = __ballot(before + up > f.target);
-        // the first lane of the wavefront whose entries cross; one of them does, up to rounding
-        if (cross && before <= f.target && lane == (int)__builtin_ctzll(cross)) {
+        const unsigned long long cross = __ballot(before + up > f.target), any = __ballot(sum > 0.0);
+        // one of the wavefronts crosses, up to rounding
+        if (cross && any && before <= f.target && lane == crossing(cross, any)) {
             int first = last;
-            double run = before + (up - sum);
+            double run = fmin(before + (up - sum), f.target);
 #pragma unroll
             for (int e = 0; e < EPV; ++e) {
                 if (run <= f.target && w[e] > 0.0) first = (int)(j - from) + e;
@@ -720,7 +726,7 @@ __global__ void __launch_bounds__(kVerifyBlock) verify_pick_k(Verify p)
     if (token < 0) {  // the entries, added up in another order, stay below what the piece's sum promised: the last that has any
         atomicMax(&lds_last, last);
         __syncthreads();
-        token = from + lds_last;
+        token = from + (lds_last > 0 ? lds_last : 0);
     }
     if (tid == 0) {
         tokens_out[at.n] = token;

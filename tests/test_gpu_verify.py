@@ -164,6 +164,39 @@ def test_borders_of_the_sums():
     assert got[0][:, 0].tolist() == [0, 1, 1, 4, 5, 6, 6, 6]
 
 
+@pytest.mark.parametrize("vocab", [256, 3000])
+@pytest.mark.parametrize("draft", [True, False])
+def test_roundings_at_borders(vocab, draft):
+    """Random numbers a few roundings from the border behind a random entry, in rows of which most has no probability, so that most
+    lanes have nothing: the token is that entry or the next one that has any."""
+    n = 2000
+    g = np.random.default_rng(vocab)
+    z = g.normal(size=(n, vocab)).astype(np.float32) * 2
+    z[g.random((n, vocab)) < 0.97] = -np.inf
+    z[:, g.integers(vocab)] = 1.0
+    p = np.exp(z.astype(np.float64))
+    if draft:  # q has all of its mass on an entry that p does not have: w = p
+        p[:, 7] = 0.0
+        z[:, 7] = -np.inf
+    c = np.cumsum(p, 1)
+    v, near = np.empty(n), []
+    for b in range(n):
+        has = np.flatnonzero(p[b])
+        i = int(g.integers(len(has)))
+        x = min(c[b, has[i]] / c[b, -1], 1 - 2.0 ** -53)
+        for _ in range(int(g.integers(5))):
+            x = np.nextafter(x, 2.0 * (b % 2))
+        v[b] = min(max(x, 0.0), 1 - 2.0 ** -53)
+        near.append({int(has[i]), int(has[min(i + 1, len(has) - 1)])})
+    target = np.zeros((n, 1 + draft, vocab), np.float32)
+    target[:, 0] = z
+    tokens, u = torch.full((n, int(draft)), 7, dtype=torch.int64).cuda(), torch.zeros((n, int(draft))).cuda()
+    got = grpo.grpo_verify_drafts(rows(torch.from_numpy(target), F32), None, tokens, u, torch.from_numpy(v).cuda())
+    assert (got[1] == 0).all()
+    out = got[0][:, 0].tolist()
+    assert [b for b in range(n) if out[b] not in near[b]] == []
+
+
 def test_ratios_at_their_borders():
     """u q < p with equality, q = 0, p = 0 and u = 0."""
     low = float("-inf")
