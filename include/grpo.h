@@ -497,6 +497,7 @@ grpo_status grpo_lmhead_loss_aux_fwd_bwd(const void *hidden, int64_t hidden_stri
  * of t is rounded from fp64.
  * drafts in [0, 64]; vocab in [1, 2^28]; batch so that the logits have no more than 2^34 entries or so (GRPO_ERR_SHAPE).  workspace: device, 256-byte aligned, at least
  * grpo_verify_workspace_bytes(...) bytes (0 for invalid sizes), contents ignored.  batch == 0 does nothing.
+ * Outputs may not overlap inputs or one another.
  * ------------------------------------------------------------------------- */
 size_t grpo_verify_workspace_bytes(int64_t batch, int64_t drafts, int64_t vocab, grpo_dtype dtype);
 grpo_status grpo_verify_drafts(const void *target_logits, int64_t target_batch_stride, int64_t target_row_stride,
@@ -602,7 +603,7 @@ grpo_status grpo_block_norm_bwd(const void *residual_out, int64_t residual_out_s
  *  weight_decay  finite.
  * Arithmetic is fp32, each operation rounded by itself, in the order printed above (sums of the norm: fp64).
  * NaN and Inf in a gradient reach the value's own parameter and moments, and through the
- * norm's coefficient all of them; they are never hidden.
+ * norm's coefficient all of them: a norm of NaN makes it NaN, one of Inf 0 (and 0 times Inf NaN).
  * ------------------------------------------------------------------------- */
 typedef struct grpo_optim_tensor {
     void *param;

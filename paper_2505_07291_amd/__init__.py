@@ -1,6 +1,7 @@
 """libgrpo for MI355X: the GRPO token-level objective with two-sided clipping
 (forward + fused backward over the full vocabulary) as hand-written gfx950 kernels
-behind a C ABI (include/grpo.h).  This package is the thin binding plus the seeded
+behind a C ABI (include/grpo.h), and beside it the verification of drafted tokens, the norms
+around a model's blocks, the gradient norm and AdamW.  This package is the thin binding plus the seeded
 synthetic workloads; it has no CPU implementation of the path."""
 from .binding import (COUNT_NAMES, GRPO_BF16, GRPO_F32, GrpoError, grpo_filter_groups,  # noqa: F401
                       grpo_group_advantages, grpo_total_rewards,

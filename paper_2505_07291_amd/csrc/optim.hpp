@@ -291,8 +291,8 @@ static __global__ void __launch_bounds__(kOptBlock) adamw_step_k(AdamW a)
     }
 }
 
-// Bound by memory: 778 million gradients in fp32, read once, take 455 us (6.8 TB/s).  14 million, which the caches may hold, take 12, of
-// them 4 the second kernel: a launch costs less here than a workgroup that waits for the others' sums.
+// Bound by memory: 778 million gradients in fp32, read once, take 457 us (6.8 TB/s).  14 million, which the caches may hold, take 12, of
+// them 4 the second kernel, which adds the workgroups' sums up.
 // Squares are exact in fp64 and summed there, each workgroup's chunks in the table's order and the workgroups' sums in theirs:
 // the same gradients always give the same norm.
 template <bool GBF16, bool WIDE>
