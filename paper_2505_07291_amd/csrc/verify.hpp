@@ -6,9 +6,9 @@
 //   then one token: the smallest j with  sum_{l <= j} w_l > v sum_l w_l,  w = max(p_n - q_n, 0), or p_n behind the last draft
 //
 // verify_rows_k forms, for the drafted positions, maxima and sums of exponentials in fp32 and is bound by reading the logits (96
-// responses with 5 drafts of 152064 bf16, 292 MB, of which the caches may hold some: 49 us, 6.0 TB/s).  That is enough for a ratio that is not within 2^-15 of its random
-// number (the others are decided in fp64), but not for the token: with sums that are off by 1e-7 the border of some of 152064 tokens lies
-// between two orders' results in one row of a hundred.
+// responses with 5 drafts of 152064 bf16, 292 MB, of which the caches may hold some: 49 us, 6.0 TB/s).  That is enough for a ratio
+// that is not within 2^-15 of its random number (the others are decided in fp64), but not for the token: with sums that are off by
+// 1e-7 the border of some of 152064 tokens lies between two orders' results in one row of a hundred.
 //
 // verify_sums_k forms in fp64 what the token needs, of row n alone: then that is one in 10^8.  It is bound by fp64 arithmetic, 19
 // instructions an exponential and nine to what it comes from and is added to, of which the GPU does 1.2e12 a second (29e12 lanes of fma, 33 to
