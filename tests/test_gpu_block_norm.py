@@ -171,6 +171,30 @@ def test_sums_over_rows(n):
         assert all(not t.any() for t in first[2:])
 
 
+def test_offsets_beyond_32_bits():
+    """Rows that lie 3 GB apart: what the same rows close together give, bit for bit."""
+    s, grads = make(11, 3, 520)
+    far = 1500000000 // 8 * 8
+
+    def apart(t):
+        big = torch.empty(2 * far + 520, dtype=BF16, device="cuda").as_strided((3, 520), (far, 1))
+        return big if t is None else big.copy_(t)
+
+    close = grpo.grpo_block_norm_fwd(**s)
+    moved = {k: apart(v) if torch.is_tensor(v) and v.dim() == 2 else v for k, v in s.items()}
+    out = dict(residual_out=apart(None), hidden=apart(None))
+    grpo.grpo_block_norm_fwd(**moved, **out)
+    assert torch.equal(out["residual_out"], close[0]) and torch.equal(out["hidden"], close[1])
+    back = {k: v for k, v in s.items() if k != "residual"}
+    close = grpo.grpo_block_norm_bwd(s["residual"], **back, **grads)
+    back = {k: v for k, v in moved.items() if k != "residual"}
+    far_grads = {k: apart(v) for k, v in grads.items()}
+    out = dict(grad_residual=apart(None), grad_block=apart(None), grad_gate=apart(None))
+    got = grpo.grpo_block_norm_bwd(moved["residual"], **back, **far_grads, **out)
+    for a, b in zip(got, close):
+        assert torch.equal(a, b)
+
+
 def test_in_place():
     for res, d in ((BF16, 776), (F32, 776), (F32, 20000)):
         s, grads = make(5, 40, d, res)

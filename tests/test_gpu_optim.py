@@ -161,6 +161,40 @@ def test_against_the_formula_in_64_bits():
     assert (off <= 2.0 ** -24 * (2 * p.abs() + 12 * u.abs() + want.abs())).all()
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_offsets_beyond_32_bits(bits):
+    """A tensor of more than 2^32 values with gradients at its ends alone: there what tensors of the ends give, zeros between."""
+    n, end = 2 ** 32 + 5000, 5000  # (the last 5000 begin with a block of 256)
+    g = torch.Generator().manual_seed(bits)
+    ends = [torch.randn(end, generator=g).to(BF16).cuda() for _ in range(2)]
+
+    def zeros(n):
+        if bits == 8:
+            m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda").view(E4M3) for _ in range(2))
+            ms, vs = (torch.zeros((n + 255) // 256, device="cuda") for _ in range(2))
+        else:
+            m, v, ms, vs = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), None, None
+        return dict(p=torch.zeros(n, dtype=BF16, device="cuda"), m=m, v=v, ms=ms, vs=vs)
+
+    def step(states, grads):
+        plan = grpo.grpo_optim_plan([t["p"] for t in states], grads, [t["m"] for t in states], [t["v"] for t in states],
+                                    exp_avg_scales=[t["ms"] for t in states], exp_avg_sq_scales=[t["vs"] for t in states])
+        norm = grpo.grpo_grad_norm(plan, 0.5)
+        grpo.grpo_adamw_step(plan, 3, 1e-2, clip=torch.tensor([1.0, 0.25], device="cuda"))
+        return norm[0].item()
+
+    big, grad = zeros(n), torch.zeros(n, dtype=BF16, device="cuda")
+    grad[:end], grad[n - end:] = ends[0], ends[1]
+    small = [zeros(end), zeros(end)]
+    assert step([big], [grad]) == pytest.approx(step(small, ends), rel=2.0 ** -23)
+    for name in ("p", "m", "v"):
+        whole = big[name].view(torch.uint8) if bits == 8 and name != "p" else big[name]
+        for part, of in ((whole[:end], small[0]), (whole[n - end:], small[1])):
+            assert torch.equal(part, of[name].view(torch.uint8) if bits == 8 and name != "p" else of[name]), name
+        for at in range(end, n - end, 2 ** 28):
+            assert not whole[at:min(at + 2 ** 28, n - end)].any(), name
+
+
 def test_one_launch_over_different_tensors():
     """Tensors of every kind in one plan."""
     models = [Model(7 + k, [300, 9000], param, grad, bits, align) for k, (param, grad, bits, align) in
